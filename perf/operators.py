@@ -304,7 +304,8 @@ def work(case):
         return {"bytes": float(sum(2 * n * e for n, e in count)), "flops": float(sum(3 * n for n, _ in count))}
     N, C, e = case["N"], case["C"], 2 if case["dtype"] == "bf16" else 4
     if op in ("norm", "dnorm"):
-        rows = (4 if op == "norm" else 3) - (0 if case["residual"] else 1) + (1 if op == "dnorm" else 0)
+        # x, residual, y, out; without the residual y is x.  y, g, dx and the residual's gradient.
+        rows = 4 if case["residual"] else 2 if op == "norm" else 3
         return {"bytes": float(rows * N * C * e + 4 * C * (2 if op == "norm" else 3)), "flops": 10.0 * N * C}
     F = case["F"]
     weights = 3 * C * F + (2 * F + C if case["bias"] else 0)
