@@ -345,6 +345,131 @@ ts3_status ts3_stack_decode(ts3_stack *s, const ts3_block_weights *blocks, void 
 ts3_status ts3_stack_feedforward(ts3_stack *s, const ts3_block_weights *blocks, int32_t l, void *x,
                                  const void *pa, int64_t n, void *xn_next, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Operators for training a pre-norm block around the layer: the gated
+ * feed-forward, the residual LayerNorm and the clipping of the gradients by
+ * their global norm.  Each keeps its operands and workspace in a handle;
+ * calls on one handle share them, so they belong on one stream (or on streams
+ * ordered by events), and a handle on one device.  A handle serves calls of
+ * any n.  As for the layer, the calls only enqueue work; create, free and
+ * the growth noted at ts3_gated_backward may synchronise. */
+
+/* Gated feed-forward over points x [n, C] with hidden width F:
+ *     a = x Wg + bg,  u = x Wu + bu,  out = (act(a) * u) Wd + bd
+ *  C         : a multiple of 16, at most 256; F from 1 to 65536 (any value).
+ *              Beyond: TS3_ERR_UNSUPPORTED.
+ *  activation: SiLU a / (1 + e^-a), or GELU a Phi(a).
+ *  io_dtype  : ts3_dtype of everything the operator takes and gives: x, out,
+ *              g, dx, weights, biases and their gradients.  TS3_BF16 computes
+ *              on bf16 matrix cores with float32 sums and rounds each hidden
+ *              value (and, in the backward, da, du, h) to bfloat16 once;
+ *              TS3_FP32 keeps every operand to float32 precision in three
+ *              bf16 parts, with their range (see ts3_desc.io_dtype). */
+typedef enum { TS3_SILU = 0, TS3_GELU = 1 } ts3_activation;
+typedef struct {
+    int32_t C, F;
+    int32_t activation;
+    int32_t io_dtype;
+} ts3_gated_desc;
+
+/* Device pointers, row-major, of the io dtype: Wg, Wu [C, F], Wd [F, C];
+ * biases bg, bu [F], bd [C] may be NULL (zero).  No alignment beyond the
+ * type's own. */
+typedef struct {
+    const void *Wg, *bg;
+    const void *Wu, *bu;
+    const void *Wd, *bd;
+} ts3_gated_weights;
+
+/* Gradients written by ts3_gated_backward (overwritten, not added to): the
+ * layouts and type of the matching weights, none NULL. */
+typedef struct {
+    void *dWg, *dbg;
+    void *dWu, *dbu;
+    void *dWd, *dbd;
+} ts3_gated_grads;
+
+typedef struct ts3_gated ts3_gated; /* opaque */
+
+/* Device bytes held from the start: the operands (about 6 C F elements, three
+ * times that many for float32) and up to 68 MB of partial sums. */
+ts3_status ts3_gated_create(const ts3_gated_desc *desc, ts3_gated **out);
+ts3_status ts3_gated_free(ts3_gated *h);
+ts3_status ts3_gated_bytes(const ts3_gated *h, int64_t *bytes);
+
+/* Lay the weights out as the kernels read them.  Needed before the first
+ * forward or backward and after every change of the weights; the arrays are
+ * not read again after the enqueued work. */
+ts3_status ts3_gated_load(ts3_gated *h, const ts3_gated_weights *w, void *stream);
+
+/* out = feed-forward of x, both [n, C], 16-byte aligned; out may be x itself.
+ * n == 0 is a no-op.  A point's result does not depend on the other points,
+ * but its rounding may depend on n: a call of few points splits the hidden
+ * units over workgroups and joins their sums in order.  BAD_STATE before the
+ * first load. */
+ts3_status ts3_gated_forward(ts3_gated *h, const void *x, int64_t n, void *out, void *stream);
+
+/* Gradients of sum(g * out) for the x and the loaded weights of the forward
+ * (which need not have run: the hidden layer is recomputed).  dx [n, C]
+ * (neither x nor g) and the weight gradients.  The points pass in tiles of `tile`
+ * (at most 2^24 are taken): a tile's da, du and h stay in a store of
+ * 3 F min(tile, n) elements between the two kernels that make and use them.
+ * The store is allocated by the first call, or a later one that needs more
+ * (this synchronises; TS3_ERR_OUT_OF_MEMORY if it does not fit), and kept.
+ * Sums over points are in a fixed order for given n and tile.  n == 0 writes
+ * zero gradients. */
+ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_t n, int64_t tile, void *dx,
+                              const ts3_gated_grads *grads, void *stream);
+
+/* Residual LayerNorm over rows of C values, C a multiple of 16 up to 512:
+ *     y = x + r,  out = (y - mean) / sqrt(var + eps) * gamma + beta
+ * (biased variance).  x, r, y, out, g, gr, dx are [n, C] of the io dtype,
+ * 16-byte aligned; gamma, beta and their gradients float32.  Statistics and
+ * sums are float32; out is that of the unrounded sum y. */
+typedef struct {
+    int32_t C;
+    int32_t io_dtype;
+    float eps; /* finite, >= 0 */
+} ts3_norm_desc;
+typedef struct ts3_norm ts3_norm; /* opaque */
+ts3_status ts3_norm_create(const ts3_norm_desc *desc, ts3_norm **out);
+ts3_status ts3_norm_free(ts3_norm *h);
+
+/* r may be NULL (y = x); y may be NULL (not wanted) or x or r; out is none of
+ * them.  n == 0 is a no-op. */
+ts3_status ts3_norm_forward(ts3_norm *h, const void *x, const void *r, const float *gamma, const float *beta,
+                            int64_t n, void *y, void *out, void *stream);
+
+/* Gradients of sum(g * out) + sum(gr * y) for the forward's y: dx [n, C], which
+ * is the gradient of x and of r alike, dgamma and dbeta [C] (overwritten).
+ * gr may be NULL (zero).  dx may be g or gr.  n == 0 writes zero dgamma and
+ * dbeta.  Column sums are in a fixed order for given n. */
+ts3_status ts3_norm_backward(ts3_norm *h, const void *y, const void *g, const void *gr, const float *gamma,
+                             int64_t n, void *dx, float *dgamma, float *dbeta, void *stream);
+
+/* Clipping by the global norm over `count` tensors (0 <= count <= 16384) of
+ * mixed types:
+ *     norm = sqrt(sum of squares of every element),  dst = src * min(1, max_norm / norm)
+ * Squares and sums are float64.  Each src is a device array of n >= 0 elements
+ * aligned to its type; dst is another of the same size, or src itself (in
+ * place: left untouched where norm <= max_norm).  No dst may overlap another
+ * tensor's src.  `norm` (device float, may be NULL) receives the norm before
+ * clipping.  max_norm > 0; +infinity only measures (and copies).  An infinite
+ * norm scales by zero (infinite elements become NaN), a NaN norm by one: the
+ * caller reads `norm` to skip such a step. */
+typedef struct {
+    const void *src;
+    void *dst;
+    int64_t n;
+    int32_t dtype; /* ts3_dtype */
+    int32_t reserved; /* 0 */
+} ts3_clip_tensor;
+typedef struct ts3_clip ts3_clip; /* opaque */
+ts3_status ts3_clip_create(ts3_clip **out);
+ts3_status ts3_clip_free(ts3_clip *h);
+ts3_status ts3_clip_gradients(ts3_clip *h, const ts3_clip_tensor *tensors, int32_t count, float max_norm,
+                              float *norm, void *stream);
+
 const char *ts3_status_string(ts3_status s);
 const char *ts3_last_error(void); /* thread-local detail of the last failure */
 

@@ -4,7 +4,8 @@ The layer runs in ``libts3.so`` (HIP kernels behind the C ABI of
 ``include/ts3.h``); ``layer.PhysicsAttention`` marshals torch tensors into it.
 Importing this package loads nothing; the library is loaded on first use.
 """
-__all__ = ["PhysicsAttention", "LayerWeights", "TransolverStack", "BlockWeights"]
+__all__ = ["PhysicsAttention", "LayerWeights", "TransolverStack", "BlockWeights", "GatedFeedForward",
+           "GatedWeights", "ResidualNorm", "GradClip"]
 
 
 def __getattr__(name):
@@ -14,4 +15,7 @@ def __getattr__(name):
     if name in ("TransolverStack", "BlockWeights"):
         from . import stack
         return getattr(stack, name)
+    if name in ("GatedFeedForward", "GatedWeights", "ResidualNorm", "GradClip"):
+        from . import train
+        return getattr(train, name)
     raise AttributeError(name)

@@ -43,6 +43,34 @@ BLOCK_EXTRA_NAMES = ("ln1_g", "ln1_b", "ln2_g", "ln2_b", "Wa", "ba", "Wb", "bb")
 class BlockWeights(ct.Structure):
     _fields_ = [("pa", Weights)] + [(n, ct.c_void_p) for n in BLOCK_EXTRA_NAMES]
 
+
+TS3_SILU, TS3_GELU = 0, 1
+
+
+class GatedDesc(ct.Structure):
+    _fields_ = [("C", ct.c_int32), ("F", ct.c_int32), ("activation", ct.c_int32), ("io_dtype", ct.c_int32)]
+
+
+GATED_NAMES = ("Wg", "bg", "Wu", "bu", "Wd", "bd")
+
+
+class GatedWeights(ct.Structure):
+    _fields_ = [(n, ct.c_void_p) for n in GATED_NAMES]
+
+
+class GatedGrads(ct.Structure):
+    _fields_ = [("d" + n, ct.c_void_p) for n in GATED_NAMES]
+
+
+class NormDesc(ct.Structure):
+    _fields_ = [("C", ct.c_int32), ("io_dtype", ct.c_int32), ("eps", ct.c_float)]
+
+
+class ClipTensor(ct.Structure):
+    _fields_ = [("src", ct.c_void_p), ("dst", ct.c_void_p), ("n", ct.c_int64), ("dtype", ct.c_int32),
+                ("reserved", ct.c_int32)]
+
+
 _P = ct.c_void_p
 # name -> (restype, argtypes); must match include/ts3.h
 SIGNATURES = {
@@ -70,6 +98,19 @@ SIGNATURES = {
     "ts3_stack_forward": (ct.c_int, [_P, ct.POINTER(BlockWeights), _P, ct.c_int64, ct.c_int64, ct.c_int64, _P]),
     "ts3_stack_decode": (ct.c_int, [_P, ct.POINTER(BlockWeights), _P, ct.c_int64, ct.c_int64, _P]),
     "ts3_stack_feedforward": (ct.c_int, [_P, ct.POINTER(BlockWeights), ct.c_int32, _P, _P, ct.c_int64, _P, _P]),
+    "ts3_gated_create": (ct.c_int, [ct.POINTER(GatedDesc), ct.POINTER(_P)]),
+    "ts3_gated_free": (ct.c_int, [_P]),
+    "ts3_gated_bytes": (ct.c_int, [_P, ct.POINTER(ct.c_int64)]),
+    "ts3_gated_load": (ct.c_int, [_P, ct.POINTER(GatedWeights), _P]),
+    "ts3_gated_forward": (ct.c_int, [_P, _P, ct.c_int64, _P, _P]),
+    "ts3_gated_backward": (ct.c_int, [_P, _P, _P, ct.c_int64, ct.c_int64, _P, ct.POINTER(GatedGrads), _P]),
+    "ts3_norm_create": (ct.c_int, [ct.POINTER(NormDesc), ct.POINTER(_P)]),
+    "ts3_norm_free": (ct.c_int, [_P]),
+    "ts3_norm_forward": (ct.c_int, [_P, _P, _P, _P, _P, ct.c_int64, _P, _P, _P]),
+    "ts3_norm_backward": (ct.c_int, [_P, _P, _P, _P, _P, ct.c_int64, _P, _P, _P, _P]),
+    "ts3_clip_create": (ct.c_int, [ct.POINTER(_P)]),
+    "ts3_clip_free": (ct.c_int, [_P]),
+    "ts3_clip_gradients": (ct.c_int, [_P, ct.POINTER(ClipTensor), ct.c_int32, ct.c_float, _P, _P]),
     "ts3_status_string": (ct.c_char_p, [ct.c_int]),
     "ts3_last_error": (ct.c_char_p, []),
 }

@@ -1410,3 +1410,4 @@ ts3_status ts3_layer_forward_noalloc(const ts3_desc *desc, const ts3_weights *w,
 }  // extern "C"
 
 #include "ts3_stack.h"
+#include "ts3_train.h"

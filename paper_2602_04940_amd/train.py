@@ -1,0 +1,207 @@
+"""Python face of libts3's training operators (include/ts3.h): the gated feed-forward,
+the residual LayerNorm and the clipping of gradients by their global norm.  Argument
+marshalling only; every step runs in the library's HIP kernels."""
+from __future__ import annotations
+
+import ctypes as ct
+
+import torch
+
+from . import _lib as L
+from .layer import _DTYPES, _ptr, _stream
+
+_ACTIVATIONS = {"silu": L.TS3_SILU, "gelu": L.TS3_GELU}
+_CODES = {t: code for code, t in _DTYPES.values()}
+
+
+class _Handle:
+    """Owns a library object: self.h, released by ts3_<kind>_free."""
+
+    _free = None
+    h = None
+
+    def close(self):
+        if self.h:
+            L.check(getattr(L.lib(), self._free)(self.h), self._free)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        self.close()
+
+    def _rows(self, t, name, n=None):
+        if not (t.is_cuda and t.dtype == self.torch_dtype and t.is_contiguous() and t.dim() == 2
+                and t.shape[1] == self.C and (n is None or t.shape[0] == n)):
+            raise ValueError(f"{name} must be a contiguous cuda {self.torch_dtype} tensor "
+                             f"[{'n' if n is None else n}, {self.C}]")
+
+    def _vector(self, t, name):
+        if not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.shape == (self.C,)):
+            raise ValueError(f"{name} must be a contiguous cuda float32 tensor [{self.C}]")
+
+
+class GatedWeights:
+    """Device copies, in the operator's type ("bf16" or "fp32"), of Wg, Wu [C, F], Wd [F, C]
+    and the biases bg, bu [F], bd [C], which may be absent.  Tensors that already are
+    contiguous device tensors of that type are used as they are, not copied."""
+
+    def __init__(self, weights: dict, dtype="bf16", device="cuda"):
+        _, self.torch_dtype = _DTYPES[dtype]
+        self.t = {}
+        for n in L.GATED_NAMES:
+            v = weights.get(n)
+            self.t[n] = v if v is None else torch.as_tensor(v).to(device=device, dtype=self.torch_dtype).contiguous()
+        for n in ("Wg", "Wu", "Wd"):
+            if self.t[n] is None:
+                raise ValueError(f"{n} is missing")
+        self.C, self.F = self.t["Wg"].shape
+        for n, shape in (("Wu", (self.C, self.F)), ("Wd", (self.F, self.C)), ("bg", (self.F,)), ("bu", (self.F,)),
+                         ("bd", (self.C,))):
+            if self.t[n] is not None and self.t[n].shape != shape:
+                raise ValueError(f"{n} must be {list(shape)}, not {list(self.t[n].shape)}")
+
+
+class GatedFeedForward(_Handle):
+    """out = (act(x Wg + bg) * (x Wu + bu)) Wd + bd for points x [n, C], and its gradient.
+
+    load() lays a GatedWeights out for the kernels: once for serving, after every change of
+    the weights in training.  Everything the operator takes and gives is of its dtype."""
+
+    _free = "ts3_gated_free"
+
+    def __init__(self, C, F, activation="silu", dtype="bf16"):
+        self.C, self.F = C, F
+        code, self.torch_dtype = _DTYPES[dtype]
+        self.desc = L.GatedDesc(C=C, F=F, activation=_ACTIVATIONS[activation], io_dtype=code)
+        h = ct.c_void_p()
+        L.check(L.lib().ts3_gated_create(ct.byref(self.desc), ct.byref(h)), "ts3_gated_create")
+        self.h = h
+
+    def bytes(self) -> int:
+        b = ct.c_int64()
+        L.check(L.lib().ts3_gated_bytes(self.h, ct.byref(b)), "ts3_gated_bytes")
+        return b.value
+
+    def load(self, w: GatedWeights):
+        if (w.C, w.F, w.torch_dtype) != (self.C, self.F, self.torch_dtype):
+            raise ValueError(f"weights of C={w.C}, F={w.F}, {w.torch_dtype} for an operator of C={self.C}, F={self.F}, "
+                             f"{self.torch_dtype}")
+        s = L.GatedWeights(**{n: (t.data_ptr() if t is not None else None) for n, t in w.t.items()})
+        L.check(L.lib().ts3_gated_load(self.h, ct.byref(s), _stream()), "ts3_gated_load")
+
+    def forward(self, x, out=None):
+        self._rows(x, "x")
+        if out is None:
+            out = torch.empty_like(x)
+        self._rows(out, "out", x.shape[0])
+        L.check(L.lib().ts3_gated_forward(self.h, _ptr(x), x.shape[0], _ptr(out), _stream()), "ts3_gated_forward")
+        return out
+
+    def backward(self, x, g, tile: int = 1 << 18, dx=None):
+        """Gradients of sum(g * out) at the loaded weights: (dx, {dWg, dbg, dWu, dbu, dWd, dbd}).
+        forward(x) need not have run; see ts3_gated_backward for `tile`."""
+        self._rows(x, "x")
+        self._rows(g, "g", x.shape[0])
+        if dx is None:
+            dx = torch.empty_like(x)
+        self._rows(dx, "dx", x.shape[0])
+        C, F = self.C, self.F
+        # one buffer, the matrices first
+        flat = torch.empty(3 * C * F + 2 * F + C, device=x.device, dtype=self.torch_dtype)
+        grads, at = {}, 0
+        for n, shape in (("dWg", (C, F)), ("dWu", (C, F)), ("dWd", (F, C)), ("dbg", (F,)), ("dbu", (F,)), ("dbd", (C,))):
+            size = shape[0] * shape[1] if len(shape) == 2 else shape[0]
+            grads[n] = flat[at:at + size].view(shape)
+            at += size
+        gs = L.GatedGrads(**{n: t.data_ptr() for n, t in grads.items()})
+        L.check(L.lib().ts3_gated_backward(self.h, _ptr(x), _ptr(g), x.shape[0], tile, _ptr(dx), ct.byref(gs),
+                                           _stream()), "ts3_gated_backward")
+        return dx, grads
+
+
+class ResidualNorm(_Handle):
+    """y = x + residual and the LayerNorm of y over C channels, and the gradient of both."""
+
+    _free = "ts3_norm_free"
+
+    def __init__(self, C, dtype="bf16", eps=1e-5):
+        self.C = C
+        code, self.torch_dtype = _DTYPES[dtype]
+        self.desc = L.NormDesc(C=C, io_dtype=code, eps=eps)
+        h = ct.c_void_p()
+        L.check(L.lib().ts3_norm_create(ct.byref(self.desc), ct.byref(h)), "ts3_norm_create")
+        self.h = h
+
+    def forward(self, x, gamma, beta, residual=None, y=None, out=None):
+        """(y, LayerNorm of y).  Without a residual, y is x itself unless a tensor is given for it."""
+        self._rows(x, "x")
+        n = x.shape[0]
+        self._vector(gamma, "gamma")
+        self._vector(beta, "beta")
+        if residual is not None:
+            self._rows(residual, "residual", n)
+            if y is None:
+                y = torch.empty_like(x)
+        if y is not None:
+            self._rows(y, "y", n)
+        if out is None:
+            out = torch.empty_like(x)
+        self._rows(out, "out", n)
+        L.check(L.lib().ts3_norm_forward(self.h, _ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), n, _ptr(y), _ptr(out),
+                                         _stream()), "ts3_norm_forward")
+        return (x if y is None else y), out
+
+    def backward(self, y, g, gamma, residual_grad=None, dx=None):
+        """Gradients of sum(g * out) + sum(residual_grad * y): (dx, dgamma, dbeta); dx is that
+        of the forward's x and of its residual alike."""
+        self._rows(y, "y")
+        n = y.shape[0]
+        self._rows(g, "g", n)
+        self._vector(gamma, "gamma")
+        if residual_grad is not None:
+            self._rows(residual_grad, "residual_grad", n)
+        if dx is None:
+            dx = torch.empty_like(y)
+        self._rows(dx, "dx", n)
+        d = torch.empty((2, self.C), device=y.device, dtype=torch.float32)
+        L.check(L.lib().ts3_norm_backward(self.h, _ptr(y), _ptr(g), _ptr(residual_grad), _ptr(gamma), n, _ptr(dx),
+                                          _ptr(d[0]), _ptr(d[1]), _stream()), "ts3_norm_backward")
+        return dx, d[0], d[1]
+
+
+class GradClip(_Handle):
+    """Scales a list of gradients (float32 and bfloat16) so that their global norm is at most
+    max_norm: clip(grads, max_norm) -> the norm before, a float32 device scalar."""
+
+    _free = "ts3_clip_free"
+
+    def __init__(self):
+        h = ct.c_void_p()
+        L.check(L.lib().ts3_clip_create(ct.byref(h)), "ts3_clip_create")
+        self.h = h
+
+    def __call__(self, grads, max_norm: float, out=None):
+        """In place, or into the tensors of `out`, one of the same size and type for each."""
+        grads = list(grads)
+        out = grads if out is None else list(out)
+        if len(out) != len(grads):
+            raise ValueError(f"{len(grads)} output tensors expected, not {len(out)}")
+        arr = (L.ClipTensor * len(grads))()
+        for a, s, d in zip(arr, grads, out):
+            for t in (s, d):
+                if not (t.is_cuda and t.dtype in _CODES and t.is_contiguous()):
+                    raise ValueError("gradients must be contiguous cuda float32 or bfloat16 tensors")
+            if s.dtype != d.dtype or s.numel() != d.numel():
+                raise ValueError("an output tensor must have its gradient's type and size")
+            a.src, a.dst, a.n, a.dtype = s.data_ptr(), d.data_ptr(), s.numel(), _CODES[s.dtype]
+        norm = torch.empty((), device=grads[0].device if grads else "cuda", dtype=torch.float32)
+        L.check(L.lib().ts3_clip_gradients(self.h, arr, len(grads), max_norm, _ptr(norm), _stream()), "ts3_clip_gradients")
+        return norm
