@@ -109,30 +109,31 @@ enum { GATED_SILU = 0, GATED_GELU = 1 };
 // t = 1 / (1 + p |z|) times e^(-z^2), z = a / sqrt 2, whose exponential is also the density's;
 // within 7.5e-8 of Phi.  That is not enough for float32, where the slope crosses zero (a =
 // -0.75): there Phi comes from erfc.  For a very negative a, e^-a overflows to infinity and s = 0.
-template <int P, bool SLOPE> __device__ __forceinline__ float gated_act(int kind, float a, float &slope) {
+template <int P, int ACT, bool SLOPE> __device__ __forceinline__ float gated_act(float a, float &slope) {
     constexpr float LOG2E = 1.44269504f;
-    if (kind == GATED_SILU) {
+    if constexpr (ACT == GATED_SILU) {
         const float s = fast_rcp(1.f + fast_exp2(-LOG2E * a));
         const float y = a * s;
         if (SLOPE) slope = s + (y - y * s);
         return y;
-    }
-    float phi, e = 0.f;
-    if (P == 1 || SLOPE) e = fast_exp2((-0.5f * LOG2E) * (a * a));
-    if constexpr (P == 1) {
-        const float t = fast_rcp(1.f + (0.3275911f * 0.70710678f) * fabsf(a));
-        float q = 0.5f * 1.061405429f;
-        q = q * t + 0.5f * -1.453152027f;
-        q = q * t + 0.5f * 1.421413741f;
-        q = q * t + 0.5f * -0.284496736f;
-        q = q * t + 0.5f * 0.254829592f;
-        q = q * t * e;
-        phi = a < 0.f ? q : 1.f - q;
     } else {
-        phi = 0.5f * erfcf(-0.70710678f * a);
+        float phi, e = 0.f;
+        if (P == 1 || SLOPE) e = fast_exp2((-0.5f * LOG2E) * (a * a));
+        if constexpr (P == 1) {
+            const float t = fast_rcp(1.f + (0.3275911f * 0.70710678f) * fabsf(a));
+            float q = 0.5f * 1.061405429f;
+            q = q * t + 0.5f * -1.453152027f;
+            q = q * t + 0.5f * 1.421413741f;
+            q = q * t + 0.5f * -0.284496736f;
+            q = q * t + 0.5f * 0.254829592f;
+            q = q * t * e;
+            phi = a < 0.f ? q : 1.f - q;
+        } else {
+            phi = 0.5f * erfcf(-0.70710678f * a);
+        }
+        if (SLOPE) slope = phi + a * (0.39894228f * e);
+        return a * phi;
     }
-    if (SLOPE) slope = phi + a * (0.39894228f * e);
-    return a * phi;
 }
 
 template <typename T> __device__ __forceinline__ float to_float(T v);
@@ -233,7 +234,7 @@ template <int BYTES, int WAVES> __device__ __forceinline__ void gated_stage(cons
 #pragma unroll
     for (int k = 0; k < (PIECES + WAVES - 1) / WAVES; ++k)
         if (PIECES % WAVES == 0 || wave + k * WAVES < PIECES)
-            dma16(src + (wave + k * WAVES) * 1024 + lane * 16, to + (wave + k * WAVES) * 1024);
+            dma16s<0>(lane * 16, src + (wave + k * WAVES) * 1024, to + (wave + k * WAVES) * 1024);
 }
 __device__ __forceinline__ void gated_sync() {
     wait_vmcnt<0>();
@@ -248,7 +249,7 @@ template <int P> __device__ __forceinline__ void lds_parts(const unsigned char *
 }
 
 // The rows of NP x MT points as operands whose columns are points: K slots 8q .. of step ks
-// are channels KI ks + 8q ...  Rows past n repeat row n - 1, channels past C are zero.
+// are channels KI ks + 8q ...  Rows past n and channels past C are zero.
 template <int P, int CP, int MT, int NP>
 __device__ __forceinline__ void gated_rows(const typename GatedIO<P>::T *x, int64_t p0, int64_t n, int C,
                                            int lane, Parts<P> (&xf)[NP][CP / Mat<MT>::KI]) {
@@ -259,28 +260,24 @@ __device__ __forceinline__ void gated_rows(const typename GatedIO<P>::T *x, int6
 #pragma unroll
         for (int ks = 0; ks < CP / Mat<MT>::KI; ++ks) {
             const int c = Mat<MT>::KI * ks + 8 * (lane / MT);
-            if (c < C) load_parts(row + c, xf[np][ks]);
-            else
+            load_parts(row + (c < C ? c : 0), xf[np][ks]);  // no branch: the loads leave together
 #pragma unroll
-                for (int s = 0; s < P; ++s) xf[np][ks].p[s] = bf16x8{};
+            for (int s = 0; s < P; ++s) xf[np][ks].p[s] = c < C && p < n ? xf[np][ks].p[s] : bf16x8{};
         }
     }
 }
 
-// r[np] += section (rows hidden, K channels) times the points' rows.
+// r[np] += section (rows hidden, K channels) times the points' rows, K step ks.
 template <int P, int CP, int MT, int NP>
-__device__ __forceinline__ void gated_hidden(const unsigned char *sec, const Parts<P> (&xf)[NP][CP / Mat<MT>::KI], int lane,
-                                             Rows32<MT> (&r)[NP]) {
-    constexpr int KS = CP / Mat<MT>::KI;
+__device__ __forceinline__ void gated_hidden(const unsigned char *sec, const Parts<P> (&xf)[NP][CP / Mat<MT>::KI], int ks,
+                                             int lane, Rows32<MT> (&r)[NP]) {
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+    for (int t = 0; t < Mat<MT>::HT; ++t) {
+        Parts<P> a;
+        lds_parts(sec, t * (CP / Mat<MT>::KI) + ks, lane, a);
 #pragma unroll
-        for (int t = 0; t < Mat<MT>::HT; ++t) {
-            Parts<P> a;
-            lds_parts(sec, t * KS + ks, lane, a);
-#pragma unroll
-            for (int np = 0; np < NP; ++np) mma_parts<MT, P>(r[np].d[t], a, xf[np][ks]);
-        }
+        for (int np = 0; np < NP; ++np) mma_parts<MT, P>(r[np].d[t], a, xf[np][ks]);
+    }
 }
 // acc[cb][np] += section (rows channels, K hidden) times hidden values.
 template <int P, int CP, int MT, int NP>
@@ -298,6 +295,18 @@ __device__ __forceinline__ void gated_channels(const unsigned char *sec, const P
 #pragma unroll
                 for (int np = 0; np < NP; ++np) mma_parts<MT, P>(acc[cb][np].d[t], a, hf[np][s]);
             }
+}
+// Order of a region of N products that read one operand each from LDS (P = 1), and PRE reads
+// before them: D operands are on their way ahead of the product that uses them.  Left to itself
+// the compiler reads one or two ahead, less than the reads' latency beside other waves' reads.
+template <int PRE, int N, int D> __device__ __forceinline__ void gated_ahead() {
+    __builtin_amdgcn_sched_group_barrier(0x100, PRE + D, 0);
+#pragma unroll
+    for (int i = 0; i < N - D; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, D, 0);
 }
 // The chunk's bias (which: 0 of the gate, 1 of the other map) as a result's first value.
 template <int MT, int NP> __device__ __forceinline__ void gated_bias(const unsigned char *bias, int which, int lane, Rows32<MT> (&r)[NP]) {
@@ -321,12 +330,14 @@ template <int P, int CP> struct GatedShape {
     static constexpr int OCC = P == 1 ? 2 : CP <= 64 ? 2 : 1;
 };
 template <int P, int CP> struct GatedShapeX {
-    static constexpr int MT = GatedShape<P, CP>::MT, NP = 1, WAVES = 4, PTS = WAVES * NP * MT;
+    static constexpr int MT = GatedShape<P, CP>::MT, WAVES = 4, PTS = WAVES * MT;
     static constexpr int OCC = P == 1 && CP <= 128 ? 2 : P == 3 && CP <= 64 ? 2 : 1;
+    static constexpr int LDS_MAX = 160 * 1024 / OCC, A = 1024 + 3 * CP * 64 * P, B = 2 * CP * 64 * P;
     // Where the five sections of a chunk do not fit LDS, they pass one by one through three slots.
-    static constexpr bool RING = 1024 + 5 * CP * 64 * P > 160 * 1024;
+    static constexpr bool RING = A + B > LDS_MAX;
     static constexpr int SLOT = 1024 + CP * 64 * P;
-    static constexpr int LDS = RING ? 3 * SLOT : 1024 + 5 * CP * 64 * P;
+    static constexpr int ASLOTS = 2 * A + B <= LDS_MAX ? 2 : 1;
+    static constexpr int LDS = RING ? 3 * SLOT : ASLOTS * A + B;
 };
 
 // out = act(x Wg + bg) * (x Wu + bu) Wd + bd.  Workgroup (block b, split s) = (id / S, id % S)
@@ -336,16 +347,16 @@ template <int P, int CP> struct GatedShapeX {
 // chunks: both products into the hidden layer, the activation, the product out of it.  (G, U)
 // and D of a chunk have one LDS slot each; each is copied while the other's products run.
 // out may be x: rows are read by their own workgroup alone, before its first barrier.
-template <int P, int CP>
+template <int P, int CP, int ACT>
 __global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
     const typename GatedIO<P>::T *x, int64_t n, int C, const unsigned char *__restrict__ ops, int nchunk, int per, int S,
-    int act, const float *__restrict__ bdp, typename GatedIO<P>::T *out,
+    const float *__restrict__ bdp, typename GatedIO<P>::T *out,
     float *__restrict__ part) {
     using Sh = GatedShape<P, CP>;
     constexpr int MT = Sh::MT, NP = Sh::NP, WAVES = Sh::WAVES;
     using M = Mat<MT>;
     using O = GatedOps<P, CP, MT>;
-    constexpr int ABYTES = 1024 + 2 * O::SEC, NV = M::NV;
+    constexpr int ABYTES = 1024 + 2 * O::SEC, NV = M::NV, AHEAD = CP > 192 ? 4 : 6;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[ABYTES + O::SEC];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int64_t blk = blockIdx.x / S;
@@ -370,8 +381,12 @@ __global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
         Rows32<MT> a[NP], u[NP];
         gated_bias<MT, NP>(sa, 0, lane, a);
         gated_bias<MT, NP>(sa, 1, lane, u);
-        gated_hidden<P, CP, MT, NP>(sa + 1024, xf, lane, a);
-        gated_hidden<P, CP, MT, NP>(sa + 1024 + O::SEC, xf, lane, u);
+#pragma unroll
+        for (int ks = 0; ks < O::KS; ++ks) {  // in turn: a product that adds to the one before it takes twice as long
+            gated_hidden<P, CP, MT, NP>(sa + 1024, xf, ks, lane, a);
+            gated_hidden<P, CP, MT, NP>(sa + 1024 + O::SEC, xf, ks, lane, u);
+        }
+        if constexpr (P == 1) gated_ahead<8, 2 * O::KS, AHEAD>();
         Parts<P> hf[NP][M::KF];
 #pragma unroll
         for (int np = 0; np < NP; ++np)
@@ -379,12 +394,13 @@ __global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
             for (int s = 0; s < M::KF; ++s) {
                 float h[8], slope;
 #pragma unroll
-                for (int t = 0; t < 8; ++t) h[t] = gated_act<P, false>(act, a[np].get(8 * s + t), slope) * u[np].get(8 * s + t);
+                for (int t = 0; t < 8; ++t) h[t] = gated_act<P, ACT, false>(a[np].get(8 * s + t), slope) * u[np].get(8 * s + t);
                 to_parts(h, hf[np][s]);
             }
         gated_sync();  // D(j) is in LDS, (G, U)(j) read by all
         if (j + 1 < j1) gated_stage<ABYTES, WAVES>(ops + (size_t)(j + 1) * O::CHUNK + O::BIAS, la, wave, lane);
         gated_channels<P, CP, MT, NP>(sb, hf, lane, acc);
+        if constexpr (P == 1) gated_ahead<0, O::CB * M::KF, AHEAD>();
         gated_sync();  // (G, U)(j+1) is in LDS, D(j) read by all
     }
 #pragma unroll
@@ -426,83 +442,83 @@ __global__ __launch_bounds__(256) void k_gated_join(const float *__restrict__ pa
     }
 }
 
+// The hidden layer of a chunk before the activation, and the gradient of its output.
+template <int MT> struct GatedHidden {
+    Rows32<MT> a[1], u[1], dh[1];
+};
+
 // dx of n points (the first nb * PTS of the store's rows), and da, du, h in the store:
-// store[m][chunk][tp][32], m = 0 da, 1 du, 2 h; rows of points past n are zero.  Grid, splits
-// and LDS slots as k_gated_fwd, with (G, U, H) and (XG, XU).
-template <int P, int CP>
+// store[m][chunk][tp][32], m = 0 da, 1 du, 2 h; rows of points past n are zero.  Grid and
+// splits as k_gated_fwd.
+// A wave's rows and sums fill half of its registers or more, so one or two waves share a
+// SIMD, and one wave alone issues its vector work beside its own products or not at all: the
+// products into the hidden layer of chunk j + 1 are interleaved with the slopes of chunk j,
+// some values after each K step, followed by chunk j's products into dx.  (G, U, H) have two
+// LDS slots where they fit, else one, (XG, XU) have one; copies are issued a phase ahead.
+template <int P, int CP, int ACT>
 __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
     const typename GatedIO<P>::T *__restrict__ x, const typename GatedIO<P>::T *__restrict__ g, int64_t n, int C,
-    const unsigned char *__restrict__ ops, int nchunk, int per, int S, int act, int64_t tp,
+    const unsigned char *__restrict__ ops, int nchunk, int per, int S, int64_t tp,
     typename GatedIO<P>::T *__restrict__ store, typename GatedIO<P>::T *__restrict__ dx, float *__restrict__ part) {
     using T = typename GatedIO<P>::T;
     using Sh = GatedShapeX<P, CP>;
-    constexpr int MT = Sh::MT, NP = Sh::NP, WAVES = Sh::WAVES;
+    constexpr int MT = Sh::MT, WAVES = Sh::WAVES;
     using M = Mat<MT>;
     using O = GatedOps<P, CP, MT>;
-    constexpr int ABYTES = 1024 + 3 * O::SEC, BBYTES = 2 * O::SEC, NV = M::NV;
-    // Stores of a chunk, issued after its copies: all of them may be in flight while those are waited for.
-    constexpr int STORES = NP * 3 * NV * (int)sizeof(T) / 16;
+    constexpr int NV = M::NV, KS = O::KS;
+    // Stores of a chunk: they are issued after its copies and may stay in flight while those are waited for.
+    constexpr int STORES = 3 * NV * (int)sizeof(T) / 16;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[Sh::LDS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int64_t blk = blockIdx.x / S;
     const int split = blockIdx.x % S;
     const int j0 = split * per, j1 = j0 + per < nchunk ? j0 + per : nchunk;
-    const int64_t p0 = blk * Sh::PTS + wave * NP * MT;
+    const int64_t p0 = blk * Sh::PTS + wave * MT, p = p0 + lane % MT;
+    const bool in = p < n;
     const uint32_t la = lds_addr(lds);
 
-    Parts<P> xf[NP][O::KS], gf[NP][O::KS];
-    Rows32<MT> acc[O::CB][NP];
-    Rows32<MT> a[NP], u[NP], dh[NP];
-    Parts<P> daf[NP][M::KF], duf[NP][M::KF];
+    Parts<P> xf[1][KS], gf[1][KS];
+    Rows32<MT> acc[O::CB][1];
+    Parts<P> daf[1][M::KF], duf[1][M::KF];
     auto start = [&]() {
-        gated_rows<P, CP, MT, NP>(x, p0, n, C, lane, xf);
-        gated_rows<P, CP, MT, NP>(g, p0, n, C, lane, gf);
+        gated_rows<P, CP, MT, 1>(x, p0, n, C, lane, xf);
+        gated_rows<P, CP, MT, 1>(g, p0, n, C, lane, gf);
 #pragma unroll
-        for (int cb = 0; cb < O::CB; ++cb)
-#pragma unroll
-            for (int np = 0; np < NP; ++np) acc[cb][np].zero();
+        for (int cb = 0; cb < O::CB; ++cb) acc[cb][0].zero();
     };
-    // da, du and h of chunk j: the next products' operands, and their rows of the store.
-    auto slopes = [&](int j) {
+    auto biases = [&](GatedHidden<MT> &c, const unsigned char *bias) {
+        gated_bias<MT, 1>(bias, 0, lane, c.a);
+        gated_bias<MT, 1>(bias, 1, lane, c.u);
+        c.dh[0].zero();
+    };
+    // K step ks of the three products into the hidden layer, from their sections at sec.
+    auto hidden = [&](GatedHidden<MT> &c, const unsigned char *sec, int ks) {
+        gated_hidden<P, CP, MT, 1>(sec, xf, ks, lane, c.a);
+        gated_hidden<P, CP, MT, 1>(sec + O::SEC, xf, ks, lane, c.u);
+        gated_hidden<P, CP, MT, 1>(sec + 2 * O::SEC, gf, ks, lane, c.dh);
+    };
+    // da, du and h of values v0 .. v1 - 1 of chunk j; each eight, as they are complete, become
+    // the next products' operands and 16 or 32 bytes of the store's rows.
+    float da[8], du[8], h[8];
+    auto slopes = [&](GatedHidden<MT> &c, int j, int v0, int v1) {
 #pragma unroll
-        for (int np = 0; np < NP; ++np) {
-            const int64_t p = p0 + np * MT + lane % MT;
-            const bool in = p < n;
-            float da[NV], du[NV], h[NV];
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                float slope;
-                const float uv = u[np].get(v), d = in ? dh[np].get(v) : 0.f;
-                const float y = gated_act<P, true>(act, a[np].get(v), slope);
-                h[v] = in ? y * uv : 0.f;
-                du[v] = d * y;
-                da[v] = d * uv * slope;
+        for (int v = v0; v < v1; ++v) {
+            float slope;
+            const float uv = c.u[0].get(v), d = c.dh[0].get(v);
+            const float y = gated_act<P, ACT, true>(c.a[0].get(v), slope);
+            h[v & 7] = in ? y * uv : 0.f;
+            du[v & 7] = d * y;
+            da[v & 7] = d * uv * slope;
+            if ((v & 7) == 7) {
+                to_parts(da, daf[0][v >> 3]);
+                to_parts(du, duf[0][v >> 3]);
+                T *const row = store + ((int64_t)j * tp + p) * 32 + NV * (lane / MT) + (v & ~7);
+                const int64_t plane = (int64_t)nchunk * tp * 32;
+                store_row<8>(row, da);
+                store_row<8>(row + plane, du);
+                store_row<8>(row + 2 * plane, h);
             }
-#pragma unroll
-            for (int s = 0; s < M::KF; ++s) {
-                float t0[8], t1[8];
-#pragma unroll
-                for (int t = 0; t < 8; ++t) {
-                    t0[t] = da[8 * s + t];
-                    t1[t] = du[8 * s + t];
-                }
-                to_parts(t0, daf[np][s]);
-                to_parts(t1, duf[np][s]);
-            }
-            asm volatile("" ::: "memory");
-            T *const row = store + ((int64_t)j * tp + p) * 32 + NV * (lane / MT);
-            const int64_t plane = (int64_t)nchunk * tp * 32;
-            store_row<NV>(row, da);
-            store_row<NV>(row + plane, du);
-            store_row<NV>(row + 2 * plane, h);
         }
-        asm volatile("" ::: "memory");
-    };
-    auto biases = [&](const unsigned char *bias) {
-        gated_bias<MT, NP>(bias, 0, lane, a);
-        gated_bias<MT, NP>(bias, 1, lane, u);
-#pragma unroll
-        for (int np = 0; np < NP; ++np) dh[np].zero();
     };
     auto barrier = [&]() {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -510,25 +526,86 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
         asm volatile("" ::: "memory");
     };
     if constexpr (!Sh::RING) {
-        const uint32_t lb = la + ABYTES;
-        const unsigned char *const sa = lds, *const sb = lds + ABYTES;
-        gated_stage<ABYTES, WAVES>(ops + (size_t)j0 * O::CHUNK + O::BIAS, la, wave, lane);
+        constexpr int AP = Sh::A / 1024 / WAVES;  // copies of (G, U, H) that every wave issues at least
+        const uint32_t lb = la + Sh::ASLOTS * Sh::A;
+        const unsigned char *const sb = lds + Sh::ASLOTS * Sh::A;
+        auto slot = [&](int j) { return Sh::ASLOTS == 2 ? ((j - j0) & 1) * Sh::A : 0; };
+        auto issue = [&](int j) { gated_stage<Sh::A, WAVES>(ops + (size_t)j * O::CHUNK + O::BIAS, la + slot(j), wave, lane); };
+        if constexpr (Sh::OCC > 1) {
+            GatedHidden<MT> c;
+            issue(j0);
+            start();
+#pragma unroll 1
+            for (int j = j0; j < j1; ++j) {
+                wait_vmcnt<0>();
+                barrier();  // (G, U, H)(j) is in LDS; chunk j - 1 is read by all
+                gated_stage<Sh::B, WAVES>(ops + (size_t)j * O::CHUNK + O::XG, lb, wave, lane);
+                const bool more = j + 1 < j1;
+                if (Sh::ASLOTS == 2 && more) issue(j + 1);
+                const unsigned char *const sec = lds + slot(j) + 1024;
+                biases(c, sec - 1024);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) hidden(c, sec, ks);
+                slopes(c, j, 0, NV);
+                asm volatile("" ::: "memory");
+                if (Sh::ASLOTS == 2 && more) wait_vmcnt<AP + STORES>();
+                else wait_vmcnt<STORES>();
+                barrier();  // (XG, XU)(j) is in LDS, (G, U, H)(j) read by all
+                if (Sh::ASLOTS == 1 && more) issue(j + 1);
+                gated_channels<P, CP, MT, 1>(sb, daf, lane, acc);
+                gated_channels<P, CP, MT, 1>(sb + O::SEC, duf, lane, acc);
+            }
+        } else {
+        // One chunk; `next`, if there is one, gets the following chunk's hidden layer.
+        auto step = [&](GatedHidden<MT> &c, GatedHidden<MT> *next, int j) {
+            wait_vmcnt<0>();
+            barrier();  // (G, U, H)(j+1) is in LDS; (G, U, H)(j) and (XG, XU)(j-1) are read by all
+            gated_stage<Sh::B, WAVES>(ops + (size_t)j * O::CHUNK + O::XG, lb, wave, lane);
+            const bool more = j + 2 < j1;
+            if (Sh::ASLOTS == 2 && more) issue(j + 2);
+            if (next) {
+                const unsigned char *const sec = lds + slot(j + 1) + 1024;
+                biases(*next, sec - 1024);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    hidden(*next, sec, ks);
+                    slopes(c, j, ks * NV / KS, (ks + 1) * NV / KS);
+                }
+            } else {
+                slopes(c, j, 0, NV);
+            }
+            asm volatile("" ::: "memory");
+            if (Sh::ASLOTS == 2 && more) wait_vmcnt<AP + STORES>();
+            else wait_vmcnt<STORES>();
+            barrier();  // (XG, XU)(j) is in LDS, (G, U, H)(j+1) read by all
+            if (Sh::ASLOTS == 1 && more) issue(j + 2);
+            gated_channels<P, CP, MT, 1>(sb, daf, lane, acc);
+            gated_channels<P, CP, MT, 1>(sb + O::SEC, duf, lane, acc);
+        };
+        GatedHidden<MT> c0, c1;
+        issue(j0);
         start();
         gated_sync();
+        if (Sh::ASLOTS == 2 && j0 + 1 < j1) issue(j0 + 1);
+        biases(c0, lds);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) hidden(c0, lds + 1024, ks);
+        if (Sh::ASLOTS == 1) {
+            barrier();  // (G, U, H)(j0) read by all
+            if (j0 + 1 < j1) issue(j0 + 1);
+        }
+        int j = j0;
 #pragma unroll 1
-        for (int j = j0; j < j1; ++j) {
-            gated_stage<BBYTES, WAVES>(ops + (size_t)j * O::CHUNK + O::XG, lb, wave, lane);
-            biases(sa);
-            gated_hidden<P, CP, MT, NP>(sa + 1024, xf, lane, a);
-            gated_hidden<P, CP, MT, NP>(sa + 1024 + O::SEC, xf, lane, u);
-            gated_hidden<P, CP, MT, NP>(sa + 1024 + 2 * O::SEC, gf, lane, dh);
-            slopes(j);
-            wait_vmcnt<STORES>();
-            barrier();  // (XG, XU)(j) is in LDS, (G, U, H)(j) read by all
-            if (j + 1 < j1) gated_stage<ABYTES, WAVES>(ops + (size_t)(j + 1) * O::CHUNK + O::BIAS, la, wave, lane);
-            gated_channels<P, CP, MT, NP>(sb, daf, lane, acc);
-            gated_channels<P, CP, MT, NP>(sb + O::SEC, duf, lane, acc);
-            gated_sync();  // (G, U, H)(j+1) is in LDS, (XG, XU)(j) read by all
+        for (; j + 2 < j1; j += 2) {
+            step(c0, &c1, j);
+            step(c1, &c0, j + 1);
+        }
+        if (j + 1 < j1) {
+            step(c0, &c1, j);
+            step(c1, nullptr, j + 1);
+        } else {
+            step(c0, nullptr, j);
+        }
         }
     } else {
         // Step i = 5 (j - j0) + q reads section q of chunk j (bias and G, U, H, XG, XU) from slot
@@ -553,42 +630,198 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
         issue(1);
         start();
         next(-1);
+        GatedHidden<MT> c;
 #pragma unroll 1
         for (int j = j0; j < j1; ++j) {
             const int i = 5 * (j - j0);
             auto slot = [&](int q) { return lds + ((i + q) % 3) * Sh::SLOT + 1024; };
             if (i + 2 < steps) issue(i + 2);
-            biases(slot(0) - 1024);
-            gated_hidden<P, CP, MT, NP>(slot(0), xf, lane, a);
+            biases(c, slot(0) - 1024);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) gated_hidden<P, CP, MT, 1>(slot(0), xf, ks, lane, c.a);
             next(i);
             if (i + 3 < steps) issue(i + 3);
-            gated_hidden<P, CP, MT, NP>(slot(1), xf, lane, u);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) gated_hidden<P, CP, MT, 1>(slot(1), xf, ks, lane, c.u);
             next(i + 1);
             if (i + 4 < steps) issue(i + 4);
-            gated_hidden<P, CP, MT, NP>(slot(2), gf, lane, dh);
-            slopes(j);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) gated_hidden<P, CP, MT, 1>(slot(2), gf, ks, lane, c.dh);
+            slopes(c, j, 0, NV);
+            asm volatile("" ::: "memory");
             next(i + 2);
             if (i + 5 < steps) issue(i + 5);
-            gated_channels<P, CP, MT, NP>(slot(3), daf, lane, acc);
+            gated_channels<P, CP, MT, 1>(slot(3), daf, lane, acc);
             next(i + 3);
             if (i + 6 < steps) issue(i + 6);
-            gated_channels<P, CP, MT, NP>(slot(4), duf, lane, acc);
+            gated_channels<P, CP, MT, 1>(slot(4), duf, lane, acc);
             next(i + 4);
         }
     }
+    if (!in) return;
 #pragma unroll
-    for (int np = 0; np < NP; ++np) {
-        const int64_t p = p0 + np * MT + lane % MT;
-        if (p >= n) continue;
+    for (int cb = 0; cb < O::CB; ++cb) {
+        const int c = 32 * cb + NV * (lane / MT);
+        float v[NV];
 #pragma unroll
-        for (int cb = 0; cb < O::CB; ++cb) {
-            const int c = 32 * cb + NV * (lane / MT);
-            float v[NV];
+        for (int i = 0; i < NV; ++i) v[i] = acc[cb][0].get(i);
+        if (S > 1) store_row<NV>(part + ((int64_t)split * n + p) * CP + c, v);
+        else if (c < C) store_row<NV>(dx + p * C + c, v);
+    }
+}
+
+// The backward of wide bfloat16 points in two kernels: their rows (x and g) and the sums of dx
+// fill a wave's registers together, so one wave per SIMD would have to do all (8,900 cycles per
+// chunk at CP = 256, of 2,560 of products); apart, two waves fit, and one's slopes run beside
+// the other's products.  dx then reads da and du back from the store.
+template <int CP> struct GatedWide {
+    static constexpr int WAVES = 4, PTS = WAVES * 32;
+    static constexpr int A = 1024 + 3 * CP * 64, B = 2 * CP * 64;
+};
+
+// da, du and h of chunks per*s .. of PTS points, as k_gated_dx leaves them in the store.  One LDS
+// slot: the next chunk is copied while the slopes of this one are computed.
+template <int CP, int ACT>
+__global__ __launch_bounds__(256, 2) void k_gated_slopes(const bf16_t *__restrict__ x, const bf16_t *__restrict__ g,
+                                                         int64_t n, int C, const unsigned char *__restrict__ ops,
+                                                         int nchunk, int per, int S, int64_t tp,
+                                                         bf16_t *__restrict__ store) {
+    using Sh = GatedWide<CP>;
+    using O = GatedOps<1, CP, 32>;
+    constexpr int WAVES = Sh::WAVES, KS = O::KS;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[Sh::A];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int64_t blk = blockIdx.x / S;
+    const int split = blockIdx.x % S;
+    const int j0 = split * per, j1 = j0 + per < nchunk ? j0 + per : nchunk;
+    const int64_t p0 = blk * Sh::PTS + wave * 32, p = p0 + lane % 32;
+    const bool in = p < n;
+    const uint32_t la = lds_addr(lds);
+    auto issue = [&](int j) { gated_stage<Sh::A, WAVES>(ops + (size_t)j * O::CHUNK + O::BIAS, la, wave, lane); };
+    auto barrier = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    issue(j0);
+    Parts<1> xf[1][KS], gf[1][KS];
+    gated_rows<1, CP, 32, 1>(x, p0, n, C, lane, xf);
+    gated_rows<1, CP, 32, 1>(g, p0, n, C, lane, gf);
+    const int64_t plane = (int64_t)nchunk * tp * 32;
+    Rows32<32> a[1], u[1], dh[1];
+    auto slopes = [&](int j) {
+        asm volatile("" ::: "memory");
+        bf16_t *const row = store + ((int64_t)j * tp + p) * 32 + 16 * (lane / 32);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] = acc[cb][np].get(i);
-            if (S > 1) store_row<NV>(part + ((int64_t)split * n + p) * CP + c, v);
-            else if (c < C) store_row<NV>(dx + p * C + c, v);
+        for (int v0 = 0; v0 < 16; v0 += 8) {
+            float da[8], du[8], h[8];
+#pragma unroll
+            for (int v = 0; v < 8; ++v) {
+                float slope;
+                const float uv = u[0].get(v0 + v), d = dh[0].get(v0 + v);
+                const float y = gated_act<1, ACT, true>(a[0].get(v0 + v), slope);
+                h[v] = in ? y * uv : 0.f;
+                du[v] = d * y;
+                da[v] = d * uv * slope;
+            }
+            store_row<8>(row + v0, da);
+            store_row<8>(row + plane + v0, du);
+            store_row<8>(row + 2 * plane + v0, h);
         }
+        asm volatile("" ::: "memory");
+    };
+#pragma unroll 1
+    for (int j = j0; j < j1; ++j) {
+        // The copies of chunk j are older than the six stores of chunk j - 1.
+        if (j > j0) wait_vmcnt<6>();
+        else wait_vmcnt<0>();
+        barrier();  // chunk j is in LDS
+        const unsigned char *const sec = lds + 1024;
+        gated_bias<32, 1>(lds, 0, lane, a);
+        gated_bias<32, 1>(lds, 1, lane, u);
+        dh[0].zero();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            gated_hidden<1, CP, 32, 1>(sec, xf, ks, lane, a);
+            gated_hidden<1, CP, 32, 1>(sec + O::SEC, xf, ks, lane, u);
+            gated_hidden<1, CP, 32, 1>(sec + 2 * O::SEC, gf, ks, lane, dh);
+        }
+        gated_ahead<8, 3 * KS, 8>();
+        barrier();  // chunk j is read by all
+        if (j + 1 < j1) issue(j + 1);
+        slopes(j);
+    }
+}
+
+// dx = da Wg^T + du Wu^T from the store, over chunks per*s ..; sums to dx or part as k_gated_fwd.
+// A chunk's da and du of a point lie in the store as the lane's operands; they are on their way
+// two chunks ahead, (XG, XU) one.
+template <int CP>
+__global__ __launch_bounds__(256, 2) void k_gated_dx_wide(int64_t n, int C, const unsigned char *__restrict__ ops,
+                                                          int nchunk, int per, int S, int64_t tp,
+                                                          const bf16_t *__restrict__ store, bf16_t *__restrict__ dx,
+                                                          float *__restrict__ part) {
+    using Sh = GatedWide<CP>;
+    using O = GatedOps<1, CP, 32>;
+    constexpr int WAVES = Sh::WAVES, SLOTS = 2, PER = Sh::B / 1024 / WAVES;
+    static_assert(Sh::B % (1024 * WAVES) == 0, "every wave issues as many copies");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[SLOTS * Sh::B];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int64_t blk = blockIdx.x / S;
+    const int split = blockIdx.x % S;
+    const int j0 = split * per, j1 = j0 + per < nchunk ? j0 + per : nchunk;
+    const int64_t p = blk * Sh::PTS + wave * 32 + lane % 32;
+    const uint32_t la = lds_addr(lds);
+    auto issue = [&](int j) {
+        gated_stage<Sh::B, WAVES>(ops + (size_t)j * O::CHUNK + O::XG, la + (j - j0) % SLOTS * Sh::B, wave, lane);
+    };
+    const int64_t plane = (int64_t)nchunk * tp * 32;
+    auto fetch = [&](int j, Parts<1> (&f)[2][1][2]) {
+        const bf16_t *const row = store + ((int64_t)j * tp + p) * 32 + 16 * (lane / 32);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) load_parts(row + m * plane + 8 * s, f[m][0][s]);
+    };
+    Rows32<32> acc[O::CB][1];
+#pragma unroll
+    for (int cb = 0; cb < O::CB; ++cb) acc[cb][0].zero();
+    Parts<1> f[3][2][1][2];
+    issue(j0);
+    fetch(j0, f[0]);
+    if (j0 + 1 < j1) fetch(j0 + 1, f[1]);
+    auto step = [&](Parts<1> (&now)[2][1][2], Parts<1> (&then)[2][1][2], int j) {
+        if (j + 1 < j1) wait_vmcnt<4>();  // da and du of chunk j + 1 may be in flight
+        else wait_vmcnt<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();  // chunk j is in LDS, chunk j - 1 read by all
+        asm volatile("" ::: "memory");
+        if (j + 1 < j1) issue(j + 1);
+        if (j + 2 < j1) fetch(j + 2, then);
+        asm volatile("" ::: "memory");
+        const unsigned char *const sec = lds + (j - j0) % SLOTS * Sh::B;
+        gated_channels<1, CP, 32, 1>(sec, now[0], lane, acc);
+        gated_channels<1, CP, 32, 1>(sec + O::SEC, now[1], lane, acc);
+        gated_ahead<0, 4 * O::CB, 6>();
+    };
+    int j = j0;
+#pragma unroll 1
+    for (; j + 2 < j1; j += 3) {
+        step(f[0], f[2], j);
+        step(f[1], f[0], j + 1);
+        step(f[2], f[1], j + 2);
+    }
+    if (j < j1) step(f[0], f[2], j);
+    if (j + 1 < j1) step(f[1], f[0], j + 1);
+    if (p >= n) return;
+#pragma unroll
+    for (int cb = 0; cb < O::CB; ++cb) {
+        const int c = 32 * cb + 16 * (lane / 32);
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = acc[cb][0].get(i);
+        if (S > 1) store_row<16>(part + ((int64_t)split * n + p) * CP + c, v);
+        else if (c < C) store_row<16>(dx + p * C + c, v);
     }
 }
 
@@ -618,118 +851,135 @@ __device__ __forceinline__ bf16x8 plane_tr(const unsigned char *plane, int r0, i
     const s16x8 v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     return __builtin_bit_cast(bf16x8, v);
 }
-// Sum of the first `count` slots.
-__device__ __forceinline__ float sum_slots(const bf16x8 &v, int count = 8) {
-    const u32x4 u = __builtin_bit_cast(u32x4, v);
-    float w[8];
+// s plus the eight slots of v.
+__device__ __forceinline__ float sum_slots(const bf16x8 &v, float s) {
+    const bf16x2 one{(__bf16)1.f, (__bf16)1.f};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        w[2 * i] = __uint_as_float(u[i] << 16);
-        w[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    }
-    if (count < 8)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = i < count ? w[i] : 0.f;
-    return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+    for (int i = 0; i < 8; i += 2) s = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{v[i], v[i + 1]}, one, s, false);
+    return s;
 }
-
 // The weight gradients of the tile's points: for m = 0 (dWg), 1 (dWu): sum of da or du times
 // x; for 2 (dWd): of h times g.  Workgroup (m, hidden block hb, split sp) with sp outermost
 // sums points per*sp .. + per - 1 (per a multiple of KP) into part[sp][m][nchunk * 32][CP] and
 // bpart[sp][m][max(nchunk * 32, CP)] (sums of da, du; for m = 2 of g), added to what is there
-// unless `first`.  Rows of x and g past n repeat row n - 1, against zeros of the store in the
-// products.  The biases' sums run over as many terms as there are points: float64.
-template <int P, int CP>
-__global__ __launch_bounds__(256, 2) void k_gated_dw(const typename GatedIO<P>::T *__restrict__ x,
-                                                     const typename GatedIO<P>::T *__restrict__ g, int64_t n, int C,
-                                                     const typename GatedIO<P>::T *__restrict__ store, int nchunk,
-                                                     int64_t tp, int64_t per, int nhb, int first,
-                                                     float *__restrict__ part, float *__restrict__ bpart) {
+// unless `first` (at the end: short chains of sums round less).  Rows past n are read from
+// `zeros` (16 bytes).
+// SUMS: column sums that the workgroup takes as it reads its operands, of the hidden columns
+// (1), of the channels (2) or none (0).  Every wave takes them, wanted or not: beside the
+// products they are free, branches around them are not.
+template <int P, int CP> struct GatedDwArgs {
+    const typename GatedIO<P>::T *x, *g, *store;
+    int64_t n, tp, per;
+    int C, nchunk, nhb, first;
+    const unsigned char *zeros;
+    float *part, *bpart;
+};
+template <int P, int CP, int SUMS>
+__device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned char *lds, int m, int hb, int sp) {
     using T = typename GatedIO<P>::T;
     using S = GatedDw<P, CP>;
     constexpr int KP = S::KP, HPL = S::HPL, PL = S::PL, CTW = S::CTW;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[S::SLOTS * S::SLOT];
+    const int64_t n = A.n, tp = A.tp, per = A.per;
+    const int C = A.C, nchunk = A.nchunk, first = A.first;
+    const T *const store = A.store;
+    const unsigned char *const zeros = A.zeros;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int wid = blockIdx.x;
-    const int hb = wid % nhb, m = wid / nhb % 3, sp = wid / (3 * nhb);
     const int hi = wave / S::WC, ci = wave % S::WC;
     const int64_t a0 = (int64_t)sp * per, a1 = a0 + per < tp ? a0 + per : tp;
     const int nk = a0 < a1 ? (int)((a1 - a0) / KP) : 0;
-    const T *const cols = m == 2 ? g : x;
+    const T *const cols = m == 2 ? A.g : A.x;
     const T *const hid = store + (int64_t)m * nchunk * tp * 32;
     const int FP = nchunk * 32, BW = FP > CP ? FP : CP;
 
-    // Piece k of a step: 16 points by one plane; lane l takes row l/4, 16 bytes (P = 1) or row
-    // l/4, 32 bytes of floats (P = 3).
-    auto source = [&](int k, int64_t p0) -> const T * {
-        const int pl = k % PL, half = k / PL;  // half: which 16 of 32 points (P = 1), or 16 of 32 columns (P = 3)
+    // Piece k of a step: 16 points by one plane of 32 columns (P = 1: half k / PL of the points) or
+    // 16 points by 16 columns (P = 3: half k / PL of the plane); lane l takes 16 bytes of row l / 4.
+    // The wave's pieces are a uniform base, which moves on with the steps, and a lane's offset.
+    const unsigned char *base[S::PER];
+    uint32_t voff[S::PER];
+    int64_t inc[S::PER];
+    constexpr int E = (int)sizeof(T);
+#pragma unroll
+    for (int i = 0; i < S::PER; ++i) {
+        const int k = wave * S::PER + i, pl = k % PL, half = k / PL;
         const int row = P == 1 ? 16 * half + (lane >> 2) : lane >> 2;
         const int col = P == 1 ? 8 * (lane & 3) : 16 * half + 4 * (lane & 3);
         if (pl < HPL) {
             int ch = hb * HPL + pl;
-            ch = ch < nchunk ? ch : nchunk - 1;
-            return hid + ((int64_t)ch * tp + p0 + row) * 32 + col;
+            ch = ch < nchunk ? ch : nchunk - 1;  // its products are not stored
+            base[i] = (const unsigned char *)(hid + ((int64_t)ch * tp + a0) * 32);
+            voff[i] = (row * 32 + col) * E;
+            inc[i] = KP * 32 * E;
+        } else {  // channels past C repeat others; their products are not stored
+            const int c = 32 * (pl - HPL) < C ? 32 * (pl - HPL) : 0;
+            base[i] = (const unsigned char *)(cols + a0 * C + c);
+            voff[i] = (row * C + (c + col < C ? col : col & 15)) * E;
+            inc[i] = (int64_t)KP * C * E;
         }
-        int64_t p = p0 + row;
-        p = p < n ? p : n - 1;
-        const int c = 32 * (pl - HPL) + col;
-        return cols + p * C + (c < C ? c : 0);  // channels past C: any, never stored
+    }
+    // Address of piece i at step k for a step that passes row n, by lane.
+    auto ragged = [&](int i, int k) {
+        const int pl = (wave * S::PER + i) % PL, half = (wave * S::PER + i) / PL;
+        const int64_t p = a0 + (int64_t)k * KP + (P == 1 ? 16 * half : 0) + (lane >> 2);
+        return pl >= HPL && p >= n ? zeros : base[i] + voff[i];
     };
     f32x16 acc[2][CTW];
     double bsum[2] = {0.0, 0.0}, gsum[CTW];
-    const bool bh = m < 2 && ci == 0, bc = m == 2 && hb == 0 && hi == 0;
-    float *const bp = bpart + ((int64_t)sp * 3 + m) * BW;
-    float *const wp = part + (((int64_t)sp * 3 + m) * FP + hb * S::HB + hi * 64) * CP + ci * CTW * 32;
+    const bool bh = SUMS == 1 && ci == 0, bc = SUMS == 2 && hi == 0;
+    float *const bp = A.bpart + ((int64_t)sp * 3 + m) * BW;
+    float *const wp = A.part + (((int64_t)sp * 3 + m) * FP + hb * S::HB + hi * 64) * CP + ci * CTW * 32;
     auto hidden_in = [&](int t) { return hb * S::HB + hi * 64 + t * 32 < FP; };
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int c = 0; c < CTW; ++c)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = 32 * t + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-                acc[t][c][r] = first || !hidden_in(t) ? 0.f : wp[(int64_t)row * CP + 32 * c + (lane & 31)];
-            }
+            for (int r = 0; r < 16; ++r) acc[t][c][r] = 0.f;
 #pragma unroll
     for (int c = 0; c < CTW; ++c) gsum[c] = 0.0;
 
-    auto products = [&](const unsigned char *slot, int64_t left) {  // points up to row n of this step's rows
+    auto step = [&](int k) {
+        const unsigned char *const slot = lds + (k % S::SLOTS) * S::SLOT;
+        float bs[2] = {0.f, 0.f}, gs[CTW];
+#pragma unroll
+        for (int c = 0; c < CTW; ++c) gs[c] = 0.f;
 #pragma unroll
         for (int r0 = 0; r0 < KP; r0 += 16) {
             Parts<P> af[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int p = 0; p < P; ++p) af[t].p[p] = plane_tr(slot + ((2 * hi + t) * P + p) * S::PLB, r0, lane);
-            if (bh)
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int p = 0; p < P; ++p) bsum[t] += sum_slots(af[t].p[p]);
+                for (int p = 0; p < P; ++p) {
+                    af[t].p[p] = plane_tr(slot + ((2 * hi + t) * P + p) * S::PLB, r0, lane);
+                    if constexpr (SUMS == 1) bs[t] = sum_slots(af[t].p[p], bs[t]);
+                }
 #pragma unroll
             for (int c = 0; c < CTW; ++c) {
                 Parts<P> bf;
 #pragma unroll
-                for (int p = 0; p < P; ++p) bf.p[p] = plane_tr(slot + ((HPL + ci * CTW + c) * P + p) * S::PLB, r0, lane);
-                if (bc) {
-                    const int64_t in = left - r0 - 8 * (lane >> 5);
-#pragma unroll
-                    for (int p = 0; p < P; ++p) gsum[c] += sum_slots(bf.p[p], in < 8 ? (int)in : 8);
+                for (int p = 0; p < P; ++p) {
+                    bf.p[p] = plane_tr(slot + ((HPL + ci * CTW + c) * P + p) * S::PLB, r0, lane);
+                    if constexpr (SUMS == 2) gs[c] = sum_slots(bf.p[p], gs[c]);
                 }
 #pragma unroll
                 for (int t = 0; t < 2; ++t) mma_parts<32, P>(acc[t][c], af[t], bf);
             }
         }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) bsum[t] += bs[t];
+#pragma unroll
+        for (int c = 0; c < CTW; ++c) gsum[c] += gs[c];
     };
     if constexpr (P == 1) {
-        const uint32_t base = lds_addr(lds);
-        auto issue = [&](int k) {
+        const uint32_t l0 = lds_addr(lds);
+        auto issue = [&](int k) {  // k = 0, 1, 2, ... in turn
+            const bool whole = a0 + (int64_t)(k + 1) * KP <= n;
 #pragma unroll
             for (int i = 0; i < S::PER; ++i) {
                 const int pc = wave * S::PER + i;
-                if (S::PIECES % 4 == 0 || pc < S::PIECES)
-                    dma16(source(pc, a0 + (int64_t)k * KP),
-                          base + (k % S::SLOTS) * S::SLOT + (pc % PL) * S::PLB + (pc / PL) * 1024);
+                const uint32_t to = l0 + (k % S::SLOTS) * S::SLOT + (pc % PL) * S::PLB + (pc / PL) * 1024;
+                if (whole) dma16s<0>(voff[i], base[i], to);
+                else dma16(ragged(i, k), to);
+                base[i] += inc[i];
             }
         };
         static_assert(S::PIECES % 4 == 0, "every wave issues as many copies");
@@ -743,14 +993,17 @@ __global__ __launch_bounds__(256, 2) void k_gated_dw(const typename GatedIO<P>::
             __builtin_amdgcn_s_barrier();  // step k is in LDS; step k - 1's slot read by all
             asm volatile("" ::: "memory");
             if (k + 2 < nk) issue(k + 2);
-            products(lds + (k % S::SLOTS) * S::SLOT, n - a0 - (int64_t)k * KP);
+            step(k);
         }
     } else {
         f32x4 st[S::PER];
-        auto fetch = [&](int k) {
+        auto fetch = [&](int k) {  // k = 0, 1, 2, ... in turn
+            const bool whole = a0 + (int64_t)(k + 1) * KP <= n;
 #pragma unroll
-            for (int i = 0; i < S::PER; ++i)
-                st[i] = *reinterpret_cast<const f32x4 *>(source(wave * S::PER + i, a0 + (int64_t)k * KP));
+            for (int i = 0; i < S::PER; ++i) {
+                st[i] = *reinterpret_cast<const f32x4 *>(whole ? base[i] + voff[i] : ragged(i, k));
+                base[i] += inc[i];
+            }
         };
         auto put = [&](int k) {
 #pragma unroll
@@ -784,20 +1037,22 @@ __global__ __launch_bounds__(256, 2) void k_gated_dw(const typename GatedIO<P>::
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();  // step k is in LDS; step k - 1's slot read by all
             asm volatile("" ::: "memory");
-            products(lds + (k % S::SLOTS) * S::SLOT, n - a0 - (int64_t)k * KP);
+            step(k);
             if (k + 1 < nk) put(k + 1);
         }
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         if (!hidden_in(t)) continue;
+        float *const to = wp + (int64_t)(32 * t + 4 * (lane >> 5)) * CP + (lane & 31);
 #pragma unroll
-        for (int c = 0; c < CTW; ++c)
+        for (int c = 0; c < CTW; ++c) {
+            if (!first)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = 32 * t + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-                wp[(int64_t)row * CP + 32 * c + (lane & 31)] = acc[t][c][r];
-            }
+                for (int r = 0; r < 16; ++r) acc[t][c][r] += to[(8 * (r >> 2) + (r & 3)) * CP + 32 * c];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) to[(8 * (r >> 2) + (r & 3)) * CP + 32 * c] = acc[t][c][r];
+        }
         if (bh) {
             const float s = (float)(bsum[t] + __shfl_xor(bsum[t], 32));
             float *const to = bp + hb * S::HB + hi * 64 + t * 32 + (lane & 31);
@@ -811,6 +1066,16 @@ __global__ __launch_bounds__(256, 2) void k_gated_dw(const typename GatedIO<P>::
             float *const to = bp + (ci * CTW + c) * 32 + (lane & 31);
             if (lane < 32) *to = first ? s : *to + s;
         }
+}
+
+template <int P, int CP> __global__ __launch_bounds__(256, 2) void k_gated_dw(const GatedDwArgs<P, CP> A) {
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[GatedDw<P, CP>::SLOTS * GatedDw<P, CP>::SLOT];
+    // The workgroups of one split, which read the same rows of x and g, share an XCD and its L2.
+    const int wid = xcd_remap(blockIdx.x, gridDim.x);
+    const int hb = wid % A.nhb, m = wid / A.nhb % 3, sp = wid / (3 * A.nhb);
+    if (m < 2) gated_dw<P, CP, 1>(A, lds, m, hb, sp);
+    else if (hb == 0) gated_dw<P, CP, 2>(A, lds, m, hb, sp);
+    else gated_dw<P, CP, 0>(A, lds, m, hb, sp);
 }
 
 // The gradients from the splits' sums, in index order: block (hidden tile of 32, channel tile

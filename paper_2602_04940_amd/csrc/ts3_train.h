@@ -150,7 +150,8 @@ ts3_status ts3_gated_create(const ts3_gated_desc *desc, ts3_gated **out) {
     ts3_status s = gated_dispatch(h, [&](auto p, auto cp) {
         constexpr int P = decltype(p)::value, CP = decltype(cp)::value;
         const int64_t ops = (int64_t)h->nchunk * GatedOps<P, CP, GatedShape<P, CP>::MT>::CHUNK;
-        const int64_t part = (int64_t)device_cu_count() * GatedShape<P, CP>::PTS * CP * 4;
+        // a round of workgroups of the kernel with the largest blocks of points
+        const int64_t part = (int64_t)device_cu_count() * std::max(GatedShape<P, CP>::PTS, GatedWide<CP>::PTS) * CP * 4;
         ts3_status st = device_alloc((void **)&h->ops, ops);
         if (st == TS3_OK) st = device_alloc((void **)&h->bd, CP * 4);
         if (st == TS3_OK) st = device_alloc((void **)&h->part, part);
@@ -216,8 +217,9 @@ ts3_status ts3_gated_forward(ts3_gated *h, const void *x, int64_t n, void *out, 
             const int64_t m = std::min<int64_t>(n - p0, MAX_WGS * PTS), nb = (m + PTS - 1) / PTS;
             const int S = gated_splits(nb, h->nchunk), per = (h->nchunk + S - 1) / S;
             T *const to = (T *)out + p0 * C;
-            hipLaunchKernelGGL((k_gated_fwd<P, CP>), dim3((unsigned)(nb * S)), dim3(256), 0, st, (const T *)x + p0 * C, m,
-                               C, h->ops, h->nchunk, per, S, h->desc.activation, h->bd, to, h->part);
+            const auto kernel = h->desc.activation == TS3_SILU ? &k_gated_fwd<P, CP, GATED_SILU> : &k_gated_fwd<P, CP, GATED_GELU>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(nb * S)), dim3(256), 0, st, (const T *)x + p0 * C, m, C, h->ops,
+                               h->nchunk, per, S, h->bd, to, h->part);
             LAUNCH_CHECK("gated forward");
             if (S > 1) {
                 hipLaunchKernelGGL((k_gated_join<P, CP>), dim3((unsigned)((m * (C / 4) + 255) / 256)), dim3(256), 0, st,
@@ -247,10 +249,13 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
         constexpr int P = decltype(p)::value, CP = decltype(cp)::value;
         using T = typename GatedIO<P>::T;
         using Dw = GatedDw<P, CP>;
-        constexpr int PTS = GatedShapeX<P, CP>::PTS;
+        constexpr bool WIDE = P == 1 && CP > 128;
+        constexpr int PTS = WIDE ? GatedWide<CP>::PTS : GatedShapeX<P, CP>::PTS;
         const int C = h->desc.C, F = h->desc.F, nchunk = h->nchunk, FP = nchunk * 32, BW = std::max(FP, CP);
         const int nhb = (FP + Dw::HB - 1) / Dw::HB;
         hipStream_t st = (hipStream_t)stream;
+        // k_gated_load leaves zeros after the 64 biases of a chunk's block.
+        const unsigned char *const zeros = h->ops + GatedOps<P, CP, GatedShape<P, CP>::MT>::BIAS + 256;
         const int64_t step = std::min(std::min(tile, GATED_TILE_MAX), std::max<int64_t>(n, 1));
         const int SP = n > 0 ? gated_point_splits<P, CP>(nchunk, step) : 0;
         if (n > 0) {
@@ -284,8 +289,19 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
             const int S = gated_splits(nb, nchunk), per = (nchunk + S - 1) / S;
             const T *const xt = (const T *)x + t0 * C, *const gt = (const T *)g + t0 * C;
             T *const dxt = (T *)dx + t0 * C;
-            hipLaunchKernelGGL((k_gated_dx<P, CP>), dim3((unsigned)(nb * S)), dim3(256), 0, st, xt, gt, m, C, h->ops,
-                               nchunk, per, S, h->desc.activation, tp, (T *)h->store, dxt, h->part);
+            const bool silu = h->desc.activation == TS3_SILU;
+            if constexpr (WIDE) {
+                const auto slopes = silu ? &k_gated_slopes<CP, GATED_SILU> : &k_gated_slopes<CP, GATED_GELU>;
+                hipLaunchKernelGGL(slopes, dim3((unsigned)(nb * S)), dim3(256), 0, st, xt, gt, m, C, h->ops, nchunk, per,
+                                   S, tp, (T *)h->store);
+                LAUNCH_CHECK("gated slopes");
+                hipLaunchKernelGGL(k_gated_dx_wide<CP>, dim3((unsigned)(nb * S)), dim3(256), 0, st, m, C, h->ops, nchunk,
+                                   per, S, tp, (const T *)h->store, dxt, h->part);
+            } else {
+                const auto kernel = silu ? &k_gated_dx<P, CP, GATED_SILU> : &k_gated_dx<P, CP, GATED_GELU>;
+                hipLaunchKernelGGL(kernel, dim3((unsigned)(nb * S)), dim3(256), 0, st, xt, gt, m, C, h->ops, nchunk, per,
+                                   S, tp, (T *)h->store, dxt, h->part);
+            }
             LAUNCH_CHECK("gated dx");
             if (S > 1) {
                 hipLaunchKernelGGL((k_gated_join<P, CP>), dim3((unsigned)((m * (C / 4) + 255) / 256)), dim3(256), 0, st,
@@ -293,8 +309,9 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
                 LAUNCH_CHECK("gated join");
             }
             const int64_t pps = ((tp + SP - 1) / SP + Dw::KP - 1) / Dw::KP * Dw::KP;
-            hipLaunchKernelGGL((k_gated_dw<P, CP>), dim3((unsigned)(3 * nhb * SP)), dim3(256), 0, st, xt, gt, m, C,
-                               (const T *)h->store, nchunk, tp, pps, nhb, t0 == 0, h->wpart, h->bpart);
+            const GatedDwArgs<P, CP> a{xt, gt, (const T *)h->store, m, tp, pps, C, nchunk, nhb, t0 == 0, zeros, h->wpart,
+                                       h->bpart};
+            hipLaunchKernelGGL((k_gated_dw<P, CP>), dim3((unsigned)(3 * nhb * SP)), dim3(256), 0, st, a);
             LAUNCH_CHECK("gated weight gradients");
         }
         hipLaunchKernelGGL((k_gated_grads<P, CP>), dim3(nchunk, (C + 31) / 32, 3), dim3(256), 0, st, h->wpart, h->bpart,
