@@ -110,7 +110,7 @@ SIGNATURES = {
     "ts3_norm_backward": (ct.c_int, [_P, _P, _P, _P, _P, ct.c_int64, _P, _P, _P, _P]),
     "ts3_clip_create": (ct.c_int, [ct.POINTER(_P)]),
     "ts3_clip_free": (ct.c_int, [_P]),
-    "ts3_clip_gradients": (ct.c_int, [_P, ct.POINTER(ClipTensor), ct.c_int32, ct.c_float, _P, _P]),
+    "ts3_clip_gradients": (ct.c_int, [_P, _P, ct.c_int32, ct.c_float, _P, _P]),
     "ts3_status_string": (ct.c_char_p, [ct.c_int]),
     "ts3_last_error": (ct.c_char_p, []),
 }

@@ -345,7 +345,8 @@ template <int P, int CP> struct GatedShapeX {
 // sums to part[s][point][CP].
 // A wave keeps its points' rows as operands and their output sums in registers, and walks the
 // chunks: both products into the hidden layer, the activation, the product out of it.  (G, U)
-// and D of a chunk have one LDS slot each; each is copied while the other's products run.
+// have one LDS slot, free for the next chunk's once every wave's products into the hidden layer
+// are done, D two where they fit.
 // out may be x: rows are read by their own workgroup alone, before its first barrier.
 template <int P, int CP, int ACT>
 __global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
@@ -357,7 +358,8 @@ __global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
     using M = Mat<MT>;
     using O = GatedOps<P, CP, MT>;
     constexpr int ABYTES = 1024 + 2 * O::SEC, NV = M::NV, AHEAD = CP > 192 ? 4 : 6;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[ABYTES + O::SEC];
+    constexpr int DSLOTS = ABYTES + 2 * O::SEC <= 80 * 1024 ? 2 : 1;  // two workgroups per compute unit
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[ABYTES + DSLOTS * O::SEC];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int64_t blk = blockIdx.x / S;
     const int split = blockIdx.x % S;
@@ -365,8 +367,12 @@ __global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
     const int64_t p0 = blk * Sh::PTS + wave * NP * MT;
     const uint32_t la = lds_addr(lds), lb = la + ABYTES;
     const unsigned char *const sa = lds, *const sb = lds + ABYTES;
+    auto slot = [&](int j) { return DSLOTS == 2 ? ((j - j0) & 1) * O::SEC : 0; };
+    auto issue_a = [&](int j) { gated_stage<ABYTES, WAVES>(ops + (size_t)j * O::CHUNK + O::BIAS, la, wave, lane); };
+    auto issue_d = [&](int j) { gated_stage<O::SEC, WAVES>(ops + (size_t)j * O::CHUNK, lb + slot(j), wave, lane); };
 
-    gated_stage<ABYTES, WAVES>(ops + (size_t)j0 * O::CHUNK + O::BIAS, la, wave, lane);
+    issue_a(j0);
+    if (DSLOTS == 2) issue_d(j0);
     Parts<P> xf[NP][O::KS];
     gated_rows<P, CP, MT, NP>(x, p0, n, C, lane, xf);
     Rows32<MT> acc[O::CB][NP];
@@ -374,10 +380,11 @@ __global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
     for (int cb = 0; cb < O::CB; ++cb)
 #pragma unroll
         for (int np = 0; np < NP; ++np) acc[cb][np].zero();
-    gated_sync();
 #pragma unroll 1
     for (int j = j0; j < j1; ++j) {
-        gated_stage<O::SEC, WAVES>(ops + (size_t)j * O::CHUNK, lb, wave, lane);
+        gated_sync();  // (G, U)(j), and with two slots D(j), are in LDS; D(j - 1) is read by all
+        if (DSLOTS == 1) issue_d(j);
+        else if (j + 1 < j1) issue_d(j + 1);
         Rows32<MT> a[NP], u[NP];
         gated_bias<MT, NP>(sa, 0, lane, a);
         gated_bias<MT, NP>(sa, 1, lane, u);
@@ -387,6 +394,11 @@ __global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
             gated_hidden<P, CP, MT, NP>(sa + 1024 + O::SEC, xf, ks, lane, u);
         }
         if constexpr (P == 1) gated_ahead<8, 2 * O::KS, AHEAD>();
+        if (DSLOTS == 1) wait_vmcnt<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();  // (G, U)(j) is read by all; with one slot, D(j) is in LDS
+        asm volatile("" ::: "memory");
+        if (j + 1 < j1) issue_a(j + 1);
         Parts<P> hf[NP][M::KF];
 #pragma unroll
         for (int np = 0; np < NP; ++np)
@@ -397,11 +409,8 @@ __global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
                 for (int t = 0; t < 8; ++t) h[t] = gated_act<P, ACT, false>(a[np].get(8 * s + t), slope) * u[np].get(8 * s + t);
                 to_parts(h, hf[np][s]);
             }
-        gated_sync();  // D(j) is in LDS, (G, U)(j) read by all
-        if (j + 1 < j1) gated_stage<ABYTES, WAVES>(ops + (size_t)(j + 1) * O::CHUNK + O::BIAS, la, wave, lane);
-        gated_channels<P, CP, MT, NP>(sb, hf, lane, acc);
+        gated_channels<P, CP, MT, NP>(sb + slot(j), hf, lane, acc);
         if constexpr (P == 1) gated_ahead<0, O::CB * M::KF, AHEAD>();
-        gated_sync();  // (G, U)(j+1) is in LDS, D(j) read by all
     }
 #pragma unroll
     for (int np = 0; np < NP; ++np) {
@@ -432,6 +441,7 @@ __global__ __launch_bounds__(256) void k_gated_join(const float *__restrict__ pa
         const int64_t p = i / (C / 4);
         const int c = (int)(i % (C / 4)) * 4;
         f32x4 v = b ? *reinterpret_cast<const f32x4 *>(b + c) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
         for (int s = 0; s < S; ++s) {
             const f32x4 w = *reinterpret_cast<const f32x4 *>(part + ((int64_t)s * n + p) * CP + c);
 #pragma unroll
@@ -477,12 +487,23 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
     const bool in = p < n;
     const uint32_t la = lds_addr(lds);
 
+    // A float32 product on the matrix cores comes out low by some 2^-28 of its terms, whatever its
+    // sign: nothing to a value, but dbu, a sum over millions of them, was off by 4e-6 of itself. So
+    // odd points' g is negated on the way in and dh back, and the sums over points lose it.
+    const uint32_t flip = P == 3 && (lane & 1) ? 0x80008000u : 0u;
+    const float sign = P == 3 && (lane & 1) ? -1.f : 1.f;
     Parts<P> xf[1][KS], gf[1][KS];
     Rows32<MT> acc[O::CB][1];
     Parts<P> daf[1][M::KF], duf[1][M::KF];
     auto start = [&]() {
         gated_rows<P, CP, MT, 1>(x, p0, n, C, lane, xf);
         gated_rows<P, CP, MT, 1>(g, p0, n, C, lane, gf);
+        if constexpr (P == 3)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int s = 0; s < P; ++s)
+                    gf[0][ks].p[s] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, gf[0][ks].p[s]) ^ flip);
 #pragma unroll
         for (int cb = 0; cb < O::CB; ++cb) acc[cb][0].zero();
     };
@@ -493,9 +514,16 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
     };
     // K step ks of the three products into the hidden layer, from their sections at sec.
     auto hidden = [&](GatedHidden<MT> &c, const unsigned char *sec, int ks) {
-        gated_hidden<P, CP, MT, 1>(sec, xf, ks, lane, c.a);
-        gated_hidden<P, CP, MT, 1>(sec + O::SEC, xf, ks, lane, c.u);
-        gated_hidden<P, CP, MT, 1>(sec + 2 * O::SEC, gf, ks, lane, c.dh);
+#pragma unroll
+        for (int t = 0; t < M::HT; ++t) {
+            Parts<P> wg, wu, wd;
+            lds_parts(sec, t * KS + ks, lane, wg);
+            lds_parts(sec + O::SEC, t * KS + ks, lane, wu);
+            lds_parts(sec + 2 * O::SEC, t * KS + ks, lane, wd);
+            mma_parts<MT, P>(c.a[0].d[t], wg, xf[0][ks]);
+            mma_parts<MT, P>(c.u[0].d[t], wu, xf[0][ks]);
+            mma_parts<MT, P>(c.dh[0].d[t], wd, gf[0][ks]);
+        }
     };
     // da, du and h of values v0 .. v1 - 1 of chunk j; each eight, as they are complete, become
     // the next products' operands and 16 or 32 bytes of the store's rows.
@@ -504,7 +532,7 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
 #pragma unroll
         for (int v = v0; v < v1; ++v) {
             float slope;
-            const float uv = c.u[0].get(v), d = c.dh[0].get(v);
+            const float uv = c.u[0].get(v), d = P == 3 ? sign * c.dh[0].get(v) : c.dh[0].get(v);
             const float y = gated_act<P, ACT, true>(c.a[0].get(v), slope);
             h[v & 7] = in ? y * uv : 0.f;
             du[v & 7] = d * y;
@@ -1096,6 +1124,7 @@ __global__ __launch_bounds__(256) void k_gated_grads(const float *__restrict__ p
     const int64_t stride = (int64_t)3 * FP * CP;
     double v[4] = {0.0, 0.0, 0.0, 0.0};
     const float *src = part + ((int64_t)m * FP + 32 * ht + r8) * CP + 32 * ct + col;
+#pragma unroll 8
     for (int s = 0; s < SP; ++s)
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] += src[s * stride + (int64_t)8 * i * CP];

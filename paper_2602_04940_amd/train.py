@@ -5,13 +5,30 @@ from __future__ import annotations
 
 import ctypes as ct
 
+import numpy as np
 import torch
 
 from . import _lib as L
-from .layer import _DTYPES, _ptr, _stream
+from .layer import _DTYPES
 
 _ACTIVATIONS = {"silu": L.TS3_SILU, "gelu": L.TS3_GELU}
 _CODES = {t: code for code, t in _DTYPES.values()}
+_dtype, _is_cuda = torch.Tensor.dtype.__get__, torch.Tensor.is_cuda.__get__
+_CLIP_ROW = np.dtype({"names": ["src", "dst", "n", "dtype", "reserved"],
+                      "formats": [np.uint64, np.uint64, np.int64, np.int32, np.int32]})  # ts3_clip_tensor
+
+
+# The current stream of a tensor's device, as an integer, without building a Stream object
+# (a microsecond of a call of ten).
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _stream(t):
+    return _raw_stream(t.device.index)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 class _Handle:
@@ -38,13 +55,16 @@ class _Handle:
         self.close()
 
     def _rows(self, t, name, n=None):
-        if not (t.is_cuda and t.dtype == self.torch_dtype and t.is_contiguous() and t.dim() == 2
-                and t.shape[1] == self.C and (n is None or t.shape[0] == n)):
+        """Checks that t is [n, C] of the operator's type; returns n."""
+        shape = t.shape
+        if not (t.is_cuda and t.dtype is self.torch_dtype and len(shape) == 2 and shape[1] == self.C
+                and (n is None or shape[0] == n) and t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous cuda {self.torch_dtype} tensor "
                              f"[{'n' if n is None else n}, {self.C}]")
+        return shape[0]
 
     def _vector(self, t, name):
-        if not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.shape == (self.C,)):
+        if not (t.is_cuda and t.dtype is torch.float32 and t.is_contiguous() and t.shape == (self.C,)):
             raise ValueError(f"{name} must be a contiguous cuda float32 tensor [{self.C}]")
 
 
@@ -95,35 +115,37 @@ class GatedFeedForward(_Handle):
             raise ValueError(f"weights of C={w.C}, F={w.F}, {w.torch_dtype} for an operator of C={self.C}, F={self.F}, "
                              f"{self.torch_dtype}")
         s = L.GatedWeights(**{n: (t.data_ptr() if t is not None else None) for n, t in w.t.items()})
-        L.check(L.lib().ts3_gated_load(self.h, ct.byref(s), _stream()), "ts3_gated_load")
+        L.check(L.lib().ts3_gated_load(self.h, ct.byref(s), _stream(w.t["Wg"])), "ts3_gated_load")
 
     def forward(self, x, out=None):
-        self._rows(x, "x")
+        n = self._rows(x, "x")
         if out is None:
             out = torch.empty_like(x)
-        self._rows(out, "out", x.shape[0])
-        L.check(L.lib().ts3_gated_forward(self.h, _ptr(x), x.shape[0], _ptr(out), _stream()), "ts3_gated_forward")
+        else:
+            self._rows(out, "out", n)
+        L.check(L.lib().ts3_gated_forward(self.h, x.data_ptr(), n, out.data_ptr(), _stream(x)), "ts3_gated_forward")
         return out
 
     def backward(self, x, g, tile: int = 1 << 18, dx=None):
         """Gradients of sum(g * out) at the loaded weights: (dx, {dWg, dbg, dWu, dbu, dWd, dbd}).
         forward(x) need not have run; see ts3_gated_backward for `tile`."""
-        self._rows(x, "x")
-        self._rows(g, "g", x.shape[0])
+        n = self._rows(x, "x")
+        self._rows(g, "g", n)
         if dx is None:
             dx = torch.empty_like(x)
-        self._rows(dx, "dx", x.shape[0])
+        else:
+            self._rows(dx, "dx", n)
         C, F = self.C, self.F
         # one buffer, the matrices first
         flat = torch.empty(3 * C * F + 2 * F + C, device=x.device, dtype=self.torch_dtype)
         grads, at = {}, 0
-        for n, shape in (("dWg", (C, F)), ("dWu", (C, F)), ("dWd", (F, C)), ("dbg", (F,)), ("dbu", (F,)), ("dbd", (C,))):
+        for name, shape in (("dWg", (C, F)), ("dWu", (C, F)), ("dWd", (F, C)), ("dbg", (F,)), ("dbu", (F,)), ("dbd", (C,))):
             size = shape[0] * shape[1] if len(shape) == 2 else shape[0]
-            grads[n] = flat[at:at + size].view(shape)
+            grads[name] = flat[at:at + size].view(shape)
             at += size
-        gs = L.GatedGrads(**{n: t.data_ptr() for n, t in grads.items()})
-        L.check(L.lib().ts3_gated_backward(self.h, _ptr(x), _ptr(g), x.shape[0], tile, _ptr(dx), ct.byref(gs),
-                                           _stream()), "ts3_gated_backward")
+        gs = L.GatedGrads(**{k: t.data_ptr() for k, t in grads.items()})
+        L.check(L.lib().ts3_gated_backward(self.h, x.data_ptr(), g.data_ptr(), n, tile, dx.data_ptr(), ct.byref(gs),
+                                           _stream(x)), "ts3_gated_backward")
         return dx, grads
 
 
@@ -142,39 +164,41 @@ class ResidualNorm(_Handle):
 
     def forward(self, x, gamma, beta, residual=None, y=None, out=None):
         """(y, LayerNorm of y).  Without a residual, y is x itself unless a tensor is given for it."""
-        self._rows(x, "x")
-        n = x.shape[0]
+        n = self._rows(x, "x")
         self._vector(gamma, "gamma")
         self._vector(beta, "beta")
         if residual is not None:
             self._rows(residual, "residual", n)
-            if y is None:
-                y = torch.empty_like(x)
         if y is not None:
             self._rows(y, "y", n)
+        elif residual is not None:
+            y = torch.empty_like(x)
         if out is None:
             out = torch.empty_like(x)
-        self._rows(out, "out", n)
-        L.check(L.lib().ts3_norm_forward(self.h, _ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), n, _ptr(y), _ptr(out),
-                                         _stream()), "ts3_norm_forward")
+        else:
+            self._rows(out, "out", n)
+        L.check(L.lib().ts3_norm_forward(self.h, x.data_ptr(), _ptr(residual), gamma.data_ptr(), beta.data_ptr(), n,
+                                         _ptr(y), out.data_ptr(), _stream(x)), "ts3_norm_forward")
         return (x if y is None else y), out
 
     def backward(self, y, g, gamma, residual_grad=None, dx=None):
         """Gradients of sum(g * out) + sum(residual_grad * y): (dx, dgamma, dbeta); dx is that
         of the forward's x and of its residual alike."""
-        self._rows(y, "y")
-        n = y.shape[0]
+        n = self._rows(y, "y")
         self._rows(g, "g", n)
         self._vector(gamma, "gamma")
         if residual_grad is not None:
             self._rows(residual_grad, "residual_grad", n)
         if dx is None:
             dx = torch.empty_like(y)
-        self._rows(dx, "dx", n)
+        else:
+            self._rows(dx, "dx", n)
         d = torch.empty((2, self.C), device=y.device, dtype=torch.float32)
-        L.check(L.lib().ts3_norm_backward(self.h, _ptr(y), _ptr(g), _ptr(residual_grad), _ptr(gamma), n, _ptr(dx),
-                                          _ptr(d[0]), _ptr(d[1]), _stream()), "ts3_norm_backward")
-        return dx, d[0], d[1]
+        dgamma, dbeta = d.unbind()
+        L.check(L.lib().ts3_norm_backward(self.h, y.data_ptr(), g.data_ptr(), _ptr(residual_grad), gamma.data_ptr(), n,
+                                          dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), _stream(y)),
+                "ts3_norm_backward")
+        return dx, dgamma, dbeta
 
 
 class GradClip(_Handle):
@@ -191,17 +215,28 @@ class GradClip(_Handle):
     def __call__(self, grads, max_norm: float, out=None):
         """In place, or into the tensors of `out`, one of the same size and type for each."""
         grads = list(grads)
-        out = grads if out is None else list(out)
-        if len(out) != len(grads):
-            raise ValueError(f"{len(grads)} output tensors expected, not {len(out)}")
-        arr = (L.ClipTensor * len(grads))()
-        for a, s, d in zip(arr, grads, out):
-            for t in (s, d):
-                if not (t.is_cuda and t.dtype in _CODES and t.is_contiguous()):
-                    raise ValueError("gradients must be contiguous cuda float32 or bfloat16 tensors")
-            if s.dtype != d.dtype or s.numel() != d.numel():
-                raise ValueError("an output tensor must have its gradient's type and size")
-            a.src, a.dst, a.n, a.dtype = s.data_ptr(), d.data_ptr(), s.numel(), _CODES[s.dtype]
+        count = len(grads)
+        place = out is None
+        out = grads if place else list(out)
+        if len(out) != count:
+            raise ValueError(f"{count} output tensors expected, not {len(out)}")
+        T = torch.Tensor
+        # The calls on every tensor are made by map: a model has hundreds.
+        dtypes, sizes = list(map(_dtype, grads)), list(map(T.numel, grads))
+        for ts in (grads,) if place else (grads, out):
+            if not (all(map(_is_cuda, ts)) and all(map(T.is_contiguous, ts))):
+                raise ValueError("gradients must be contiguous cuda float32 or bfloat16 tensors")
+        if not (set(dtypes) <= _CODES.keys()):
+            raise ValueError("gradients must be contiguous cuda float32 or bfloat16 tensors")
+        if not place and (dtypes != list(map(_dtype, out)) or sizes != list(map(T.numel, out))):
+            raise ValueError("an output tensor must have its gradient's type and size")
+        table = np.empty(count, dtype=_CLIP_ROW)
+        table["src"] = list(map(T.data_ptr, grads))
+        table["dst"] = table["src"] if place else list(map(T.data_ptr, out))
+        table["n"] = sizes
+        table["dtype"] = list(map(_CODES.__getitem__, dtypes))
+        table["reserved"] = 0
         norm = torch.empty((), device=grads[0].device if grads else "cuda", dtype=torch.float32)
-        L.check(L.lib().ts3_clip_gradients(self.h, arr, len(grads), max_norm, _ptr(norm), _stream()), "ts3_clip_gradients")
+        L.check(L.lib().ts3_clip_gradients(self.h, table.ctypes.data, count, max_norm, norm.data_ptr(), _stream(norm)),
+                "ts3_clip_gradients")
         return norm
