@@ -1,13 +1,17 @@
-"""Compile the gfx950 HIP library ``libts3.so`` in-tree with hipcc."""
+"""Compile the gfx950 HIP library ``libts3.so`` and the binding's tensor-table module
+``_tensors.so`` in-tree."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(PKG, "csrc", "ts3.hip")
 LIB = os.path.join(PKG, "libts3.so")
+TENSORS_SRC = os.path.join(PKG, "csrc", "tensors.cpp")
+TENSORS = os.path.join(PKG, "_tensors.so")
 
 HIP_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -23,17 +27,31 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found (ROCm is required to build libts3.so)")
 
 
+def tensors_command(out: str) -> list[str]:
+    """Host code against this Python and this torch: their headers, and torch's libraries by path."""
+    import torch
+    from torch.utils import cpp_extension
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    include = [sysconfig.get_paths()["include"], *cpp_extension.include_paths()]
+    return [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *["-I" + p for p in include], "-o", out,
+            TENSORS_SRC, "-L" + libs, "-Wl,-rpath," + libs, "-ltorch_python", "-ltorch_cpu", "-lc10"]
+
+
 def build_library(verbose: bool = False) -> str:
-    """Always recompiles; writes to a temporary name and renames on success."""
-    tmp = LIB + ".tmp"
-    cmd = [hipcc(), *HIP_FLAGS, "-o", tmp, SRC]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    msgs = "\n".join(l for l in (r.stdout + r.stderr).splitlines() if "packed-fp32-ops" not in l)
-    if r.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({r.returncode}):\n{' '.join(cmd)}\n{msgs}")
-    if verbose and msgs.strip():
-        print(msgs)
+    """Always recompiles both; writes to temporary names and renames on success."""
+    tmp, tensors_tmp = LIB + ".tmp", TENSORS + ".tmp"
+    cmds = [[hipcc(), *HIP_FLAGS, "-o", tmp, SRC], tensors_command(tensors_tmp)]
+    jobs = [subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) for c in cmds]
+    outs = [j.communicate()[0] for j in jobs]
+    for cmd, job, out in zip(cmds, jobs, outs):
+        msgs = "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l)
+        if job.returncode != 0:
+            raise RuntimeError(f"{os.path.basename(cmd[0])} failed ({job.returncode}):\n{' '.join(cmd)}\n{msgs}")
+        if verbose and msgs.strip():
+            print(msgs)
     os.replace(tmp, LIB)
+    os.replace(tensors_tmp, TENSORS)
     return LIB
 
 

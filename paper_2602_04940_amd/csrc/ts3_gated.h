@@ -327,7 +327,7 @@ template <int MT, int NP> __device__ __forceinline__ void gated_bias(const unsig
 // float32 points fill the registers with 16 points per wave in the backward (MT = 16).
 template <int P, int CP> struct GatedShape {
     static constexpr int MT = P == 3 && CP > 128 ? 16 : 32, NP = 32 / MT, WAVES = 4, PTS = WAVES * NP * MT;
-    static constexpr int OCC = P == 1 ? 2 : CP <= 64 ? 2 : 1;
+    static constexpr int OCC = P == 1 || CP <= 128 ? 2 : 1;
 };
 template <int P, int CP> struct GatedShapeX {
     static constexpr int MT = GatedShape<P, CP>::MT, WAVES = 4, PTS = WAVES * MT;
@@ -347,32 +347,42 @@ template <int P, int CP> struct GatedShapeX {
 // chunks: both products into the hidden layer, the activation, the product out of it.  (G, U)
 // have one LDS slot, free for the next chunk's once every wave's products into the hidden layer
 // are done, D two where they fit.
+// HW = 2, for calls that do not fill the chip: twice the waves on the same points, the second
+// half on every other chunk, its sums added through LDS at the end.
 // out may be x: rows are read by their own workgroup alone, before its first barrier.
-template <int P, int CP, int ACT>
-__global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
+template <int P, int CP, int ACT, int HW>
+__global__ __launch_bounds__(256 * HW, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
     const typename GatedIO<P>::T *x, int64_t n, int C, const unsigned char *__restrict__ ops, int nchunk, int per, int S,
-    const float *__restrict__ bdp, typename GatedIO<P>::T *out,
-    float *__restrict__ part) {
+    const float *__restrict__ bdp, typename GatedIO<P>::T *out, float *__restrict__ part) {
     using Sh = GatedShape<P, CP>;
     constexpr int MT = Sh::MT, NP = Sh::NP, WAVES = Sh::WAVES;
     using M = Mat<MT>;
     using O = GatedOps<P, CP, MT>;
     constexpr int ABYTES = 1024 + 2 * O::SEC, NV = M::NV, AHEAD = CP > 192 ? 4 : 6;
     constexpr int DSLOTS = ABYTES + 2 * O::SEC <= 80 * 1024 ? 2 : 1;  // two workgroups per compute unit
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[ABYTES + DSLOTS * O::SEC];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    constexpr int HALF = ABYTES + DSLOTS * O::SEC, SUMS = HW == 2 ? WAVES * NP * MT * CP * 4 : 0;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[HW * HALF > SUMS ? HW * HALF : SUMS];
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int wave = wid % WAVES, half = wid / WAVES;
     const int64_t blk = blockIdx.x / S;
     const int split = blockIdx.x % S;
     const int j0 = split * per, j1 = j0 + per < nchunk ? j0 + per : nchunk;
     const int64_t p0 = blk * Sh::PTS + wave * NP * MT;
-    const uint32_t la = lds_addr(lds), lb = la + ABYTES;
-    const unsigned char *const sa = lds, *const sb = lds + ABYTES;
-    auto slot = [&](int j) { return DSLOTS == 2 ? ((j - j0) & 1) * O::SEC : 0; };
-    auto issue_a = [&](int j) { gated_stage<ABYTES, WAVES>(ops + (size_t)j * O::CHUNK + O::BIAS, la, wave, lane); };
-    auto issue_d = [&](int j) { gated_stage<O::SEC, WAVES>(ops + (size_t)j * O::CHUNK, lb + slot(j), wave, lane); };
+    const uint32_t la = lds_addr(lds) + half * HALF, lb = la + ABYTES;
+    const unsigned char *const sa = lds + half * HALF, *const sb = sa + ABYTES;
+    auto slot = [&](int i) { return DSLOTS == 2 ? (i & 1) * O::SEC : 0; };  // of the half's i-th chunk
+    auto issue_a = [&](int i) {
+        gated_stage<ABYTES, WAVES>(ops + (size_t)(j0 + HW * i + half) * O::CHUNK + O::BIAS, la, wave, lane);
+    };
+    auto issue_d = [&](int i) {
+        gated_stage<O::SEC, WAVES>(ops + (size_t)(j0 + HW * i + half) * O::CHUNK, lb + slot(i), wave, lane);
+    };
+    const int steps = (j1 - j0 + HW - 1) / HW, mine = (j1 - j0 - half + HW - 1) / HW;  // the half's own chunks
 
-    issue_a(j0);
-    if (DSLOTS == 2) issue_d(j0);
+    if (mine > 0) {
+        issue_a(0);
+        if (DSLOTS == 2) issue_d(0);
+    }
     Parts<P> xf[NP][O::KS];
     gated_rows<P, CP, MT, NP>(x, p0, n, C, lane, xf);
     Rows32<MT> acc[O::CB][NP];
@@ -380,11 +390,20 @@ __global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
     for (int cb = 0; cb < O::CB; ++cb)
 #pragma unroll
         for (int np = 0; np < NP; ++np) acc[cb][np].zero();
+    auto barrier = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
 #pragma unroll 1
-    for (int j = j0; j < j1; ++j) {
-        gated_sync();  // (G, U)(j), and with two slots D(j), are in LDS; D(j - 1) is read by all
-        if (DSLOTS == 1) issue_d(j);
-        else if (j + 1 < j1) issue_d(j + 1);
+    for (int i = 0; i < steps; ++i) {
+        gated_sync();  // (G, U), and with two slots D, of chunk i are in LDS; D of chunk i - 1 is read by all
+        if (HW == 2 && i >= mine) {
+            barrier();
+            continue;
+        }
+        if (DSLOTS == 1) issue_d(i);
+        else if (i + 1 < mine) issue_d(i + 1);
         Rows32<MT> a[NP], u[NP];
         gated_bias<MT, NP>(sa, 0, lane, a);
         gated_bias<MT, NP>(sa, 1, lane, u);
@@ -395,10 +414,8 @@ __global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
         }
         if constexpr (P == 1) gated_ahead<8, 2 * O::KS, AHEAD>();
         if (DSLOTS == 1) wait_vmcnt<0>();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();  // (G, U)(j) is read by all; with one slot, D(j) is in LDS
-        asm volatile("" ::: "memory");
-        if (j + 1 < j1) issue_a(j + 1);
+        barrier();  // (G, U) of chunk i are read by all; with one slot, D is in LDS
+        if (i + 1 < mine) issue_a(i + 1);
         Parts<P> hf[NP][M::KF];
 #pragma unroll
         for (int np = 0; np < NP; ++np)
@@ -409,8 +426,33 @@ __global__ __launch_bounds__(256, (GatedShape<P, CP>::OCC)) void k_gated_fwd(
                 for (int t = 0; t < 8; ++t) h[t] = gated_act<P, ACT, false>(a[np].get(8 * s + t), slope) * u[np].get(8 * s + t);
                 to_parts(h, hf[np][s]);
             }
-        gated_channels<P, CP, MT, NP>(sb + slot(j), hf, lane, acc);
+        gated_channels<P, CP, MT, NP>(sb + slot(i), hf, lane, acc);
         if constexpr (P == 1) gated_ahead<0, O::CB * M::KF, AHEAD>();
+    }
+    if constexpr (HW == 2) {
+        float *const sums = reinterpret_cast<float *>(lds) + wave * (NP * MT * CP) + lane * 4;
+        barrier();  // the last operands are read by all
+        if (half == 1)
+#pragma unroll
+            for (int cb = 0; cb < O::CB; ++cb)
+#pragma unroll
+                for (int np = 0; np < NP; ++np)
+#pragma unroll
+                    for (int v = 0; v < NV; v += 4)
+                        *reinterpret_cast<f32x4 *>(sums + ((cb * NP + np) * NV + v) * 64) =
+                            f32x4{acc[cb][np].get(v), acc[cb][np].get(v + 1), acc[cb][np].get(v + 2), acc[cb][np].get(v + 3)};
+        barrier();
+        if (half == 1) return;
+#pragma unroll
+        for (int cb = 0; cb < O::CB; ++cb)
+#pragma unroll
+            for (int np = 0; np < NP; ++np)
+#pragma unroll
+                for (int v = 0; v < NV; v += 4) {
+                    const f32x4 w = *reinterpret_cast<const f32x4 *>(sums + ((cb * NP + np) * NV + v) * 64);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) acc[cb][np].set(v + t, acc[cb][np].get(v + t) + w[t]);
+                }
     }
 #pragma unroll
     for (int np = 0; np < NP; ++np) {

@@ -41,11 +41,15 @@ template <typename F> auto gated_dispatch(const ts3_gated *h, F fn) {
     return h->P == 1 ? with(ic<1>{}) : with(ic<3>{});
 }
 
-// Workgroups per hidden split: a call of nb blocks of points splits the chunks so that about
-// a round of compute units is at work.
-int gated_splits(int64_t nb, int nchunk) {
-    const int64_t s = std::max<int64_t>(1, device_cu_count() / std::max<int64_t>(nb, 1));
-    const int per = (int)((nchunk + std::min<int64_t>(s, nchunk) - 1) / std::min<int64_t>(s, nchunk));
+// Splits of the hidden units over workgroups, for a call of n points in nb blocks that leaves
+// compute units idle.  S splits take chunks / S steps of t us (what one workgroup alone on its
+// compute unit takes: 0.5 us and 5 ns per channel, 18 in float32), and write and read S sums of
+// n CP floats at 1.9 TB/s together: the sum of both is least at S = sqrt(chunks t / sums).
+int gated_splits(int64_t n, int64_t nb, int nchunk, int P, int CP) {
+    const double t = 0.5 + (P == 1 ? 0.005 : 0.018) * CP, sums = (double)n * CP * 4 / 1.9e6;
+    const int64_t best = (int64_t)std::ceil(std::sqrt(nchunk * t / sums));
+    const int64_t s = std::max<int64_t>(1, std::min(std::min<int64_t>(best, nchunk), device_cu_count() / std::max<int64_t>(nb, 1)));
+    const int per = (int)((nchunk + s - 1) / s);
     return (nchunk + per - 1) / per;
 }
 
@@ -215,11 +219,20 @@ ts3_status ts3_gated_forward(ts3_gated *h, const void *x, int64_t n, void *out, 
         hipStream_t st = (hipStream_t)stream;
         for (int64_t p0 = 0; p0 < n; p0 += MAX_WGS * PTS) {
             const int64_t m = std::min<int64_t>(n - p0, MAX_WGS * PTS), nb = (m + PTS - 1) / PTS;
-            const int S = gated_splits(nb, h->nchunk), per = (h->nchunk + S - 1) / S;
+            const int S = gated_splits(m, nb, h->nchunk, P, CP), per = (h->nchunk + S - 1) / S;
             T *const to = (T *)out + p0 * C;
-            const auto kernel = h->desc.activation == TS3_SILU ? &k_gated_fwd<P, CP, GATED_SILU> : &k_gated_fwd<P, CP, GATED_GELU>;
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(nb * S)), dim3(256), 0, st, (const T *)x + p0 * C, m, C, h->ops,
-                               h->nchunk, per, S, h->bd, to, h->part);
+            const bool silu = h->desc.activation == TS3_SILU;
+            auto launch = [&](auto hw) {
+                constexpr int HW = decltype(hw)::value;
+                const auto kernel = silu ? &k_gated_fwd<P, CP, GATED_SILU, HW> : &k_gated_fwd<P, CP, GATED_GELU, HW>;
+                hipLaunchKernelGGL(kernel, dim3((unsigned)(nb * S)), dim3(256 * HW), 0, st, (const T *)x + p0 * C, m, C,
+                                   h->ops, h->nchunk, per, S, h->bd, to, h->part);
+            };
+            // One workgroup per compute unit or none: two waves per SIMD on the same points.
+            if constexpr (GatedShape<P, CP>::OCC == 2)
+                if (per > 1 && nb * S <= device_cu_count()) launch(ic<2>{});
+                else launch(ic<1>{});
+            else launch(ic<1>{});
             LAUNCH_CHECK("gated forward");
             if (S > 1) {
                 hipLaunchKernelGGL((k_gated_join<P, CP>), dim3((unsigned)((m * (C / 4) + 255) / 256)), dim3(256), 0, st,
@@ -286,7 +299,7 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
         }
         for (int64_t t0 = 0; t0 < n; t0 += step) {
             const int64_t m = std::min(step, n - t0), nb = (m + PTS - 1) / PTS, tp = nb * PTS;
-            const int S = gated_splits(nb, nchunk), per = (nchunk + S - 1) / S;
+            const int S = gated_splits(m, nb, nchunk, P, CP), per = (nchunk + S - 1) / S;
             const T *const xt = (const T *)x + t0 * C, *const gt = (const T *)g + t0 * C;
             T *const dxt = (T *)dx + t0 * C;
             const bool silu = h->desc.activation == TS3_SILU;

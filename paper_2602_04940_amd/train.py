@@ -5,17 +5,12 @@ from __future__ import annotations
 
 import ctypes as ct
 
-import numpy as np
 import torch
 
 from . import _lib as L
 from .layer import _DTYPES
 
 _ACTIVATIONS = {"silu": L.TS3_SILU, "gelu": L.TS3_GELU}
-_CODES = {t: code for code, t in _DTYPES.values()}
-_dtype, _is_cuda = torch.Tensor.dtype.__get__, torch.Tensor.is_cuda.__get__
-_CLIP_ROW = np.dtype({"names": ["src", "dst", "n", "dtype", "reserved"],
-                      "formats": [np.uint64, np.uint64, np.int64, np.int32, np.int32]})  # ts3_clip_tensor
 
 
 # The current stream of a tensor's device, as an integer, without building a Stream object
@@ -208,35 +203,20 @@ class GradClip(_Handle):
     _free = "ts3_clip_free"
 
     def __init__(self):
+        try:
+            from . import _tensors
+        except ImportError as e:
+            raise RuntimeError("_tensors.so is missing or unusable: build it with __graft_entry__.build()") from e
+        self._table = _tensors.clip_table
         h = ct.c_void_p()
         L.check(L.lib().ts3_clip_create(ct.byref(h)), "ts3_clip_create")
         self.h = h
 
     def __call__(self, grads, max_norm: float, out=None):
-        """In place, or into the tensors of `out`, one of the same size and type for each."""
-        grads = list(grads)
-        count = len(grads)
-        place = out is None
-        out = grads if place else list(out)
-        if len(out) != count:
-            raise ValueError(f"{count} output tensors expected, not {len(out)}")
-        T = torch.Tensor
-        # The calls on every tensor are made by map: a model has hundreds.
-        dtypes, sizes = list(map(_dtype, grads)), list(map(T.numel, grads))
-        for ts in (grads,) if place else (grads, out):
-            if not (all(map(_is_cuda, ts)) and all(map(T.is_contiguous, ts))):
-                raise ValueError("gradients must be contiguous cuda float32 or bfloat16 tensors")
-        if not (set(dtypes) <= _CODES.keys()):
-            raise ValueError("gradients must be contiguous cuda float32 or bfloat16 tensors")
-        if not place and (dtypes != list(map(_dtype, out)) or sizes != list(map(T.numel, out))):
-            raise ValueError("an output tensor must have its gradient's type and size")
-        table = np.empty(count, dtype=_CLIP_ROW)
-        table["src"] = list(map(T.data_ptr, grads))
-        table["dst"] = table["src"] if place else list(map(T.data_ptr, out))
-        table["n"] = sizes
-        table["dtype"] = list(map(_CODES.__getitem__, dtypes))
-        table["reserved"] = 0
-        norm = torch.empty((), device=grads[0].device if grads else "cuda", dtype=torch.float32)
-        L.check(L.lib().ts3_clip_gradients(self.h, table.ctypes.data, count, max_norm, norm.data_ptr(), _stream(norm)),
+        """grads, a list: in place, or into the tensors of the list `out`, one of the same size and
+        type for each."""
+        table, device = self._table(grads, out)
+        norm = torch.empty((), device="cuda" if device < 0 else device, dtype=torch.float32)
+        L.check(L.lib().ts3_clip_gradients(self.h, table, len(grads), max_norm, norm.data_ptr(), _stream(norm)),
                 "ts3_clip_gradients")
         return norm

@@ -77,3 +77,12 @@ def test_python_faces_check_their_tensors():
         GatedWeights(dict(w, bg=torch.zeros(16)), "fp32", "cpu")
     with pytest.raises(KeyError):
         GatedWeights(w, "fp16", "cpu")
+
+
+def test_tensor_tables_are_refused_before_any_device_call():
+    from paper_2602_04940_amd import _tensors
+    assert _tensors.clip_table([], None) == (b"", -1)
+    for grads, out, error in (([torch.zeros(3)], None, ValueError), ([3.0], None, TypeError), ([], [torch.zeros(1)], ValueError),
+                              (None, None, TypeError), ([], 5, TypeError)):
+        with pytest.raises(error):
+            _tensors.clip_table(grads, out)
