@@ -340,9 +340,54 @@ template <int P, int CP> struct GatedShapeX {
     static constexpr int LDS = RING ? 3 * SLOT : ASLOTS * A + B;
 };
 
+// Sums of a workgroup that takes a split of the hidden units: sheet (split * nb + block) of
+// part, 16 bytes of every lane after another as they lie in the registers; of the `points`
+// points of the wave that there are.
+template <int CP, int MT, int NP>
+__device__ __forceinline__ void gated_put_sums(const Rows32<MT> (&acc)[CP / 32][NP], float *sheet, int wave, int lane,
+                                               int64_t points) {
+    constexpr int NV = Mat<MT>::NV;
+    float *const to = sheet + wave * (NP * MT * CP) + lane * 4;
+#pragma unroll
+    for (int np = 0; np < NP; ++np)
+        if (np * MT + lane % MT < points)
+#pragma unroll
+            for (int cb = 0; cb < CP / 32; ++cb)
+#pragma unroll
+            for (int v = 0; v < NV; v += 4)
+                *reinterpret_cast<f32x4 *>(to + ((cb * NP + np) * NV + v) * 64) =
+                    f32x4{acc[cb][np].get(v), acc[cb][np].get(v + 1), acc[cb][np].get(v + 2), acc[cb][np].get(v + 3)};
+}
+
+// out = b + the splits' sums, in the order of the splits; b may be NULL.  A thread takes four
+// channels of a point that one lane held.  Grid: a wave for each of nb * PTS * CP / 256 such pieces.
+template <int P, int CP, int MT, int NP>
+__global__ __launch_bounds__(256) void k_gated_join(const float *__restrict__ part, int64_t n, int C, int S, int nb,
+                                                    const float *__restrict__ b, typename GatedIO<P>::T *__restrict__ out) {
+    constexpr int NV = Mat<MT>::NV, V4 = NV / 4, CB = CP / 32, PTS = 4 * NP * MT;
+    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, piece = (int)(w % (V4 * NP * CB));
+    const int v = piece % V4 * 4, np = piece / V4 % NP, cb = piece / (V4 * NP), wave = (int)(w / (V4 * NP * CB) % 4);
+    const int64_t blk = w / (V4 * NP * CB * 4), p = blk * PTS + (wave * NP + np) * MT + lane % MT;
+    const int c = 32 * cb + NV * (lane / MT) + v;
+    if (blk >= nb || p >= n || c >= C) return;
+    f32x4 sum = b ? *reinterpret_cast<const f32x4 *>(b + c) : f32x4{0.f, 0.f, 0.f, 0.f};
+    const float *src = part + blk * PTS * CP + wave * (NP * MT * CP) + ((cb * NP + np) * NV + v) * 64 + lane * 4;
+#pragma unroll 8
+    for (int s = 0; s < S; ++s) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(src + (int64_t)s * nb * PTS * CP);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sum[t] += x[t];
+    }
+    typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+    if constexpr (P == 3) *reinterpret_cast<f32x4 *>(out + p * C + c) = sum;
+    else
+        *reinterpret_cast<bf16x4 *>(out + p * C + c) = bf16x4{(__bf16)sum[0], (__bf16)sum[1], (__bf16)sum[2], (__bf16)sum[3]};
+}
+
 // out = act(x Wg + bg) * (x Wu + bu) Wd + bd.  Workgroup (block b, split s) = (id / S, id % S)
 // takes PTS points and chunks per*s .. of the hidden units; with S = 1 it writes out, else its
-// sums to part[s][point][CP].
+// sums to sheet (s, b) of part.
 // A wave keeps its points' rows as operands and their output sums in registers, and walks the
 // chunks: both products into the hidden layer, the activation, the product out of it.  (G, U)
 // have one LDS slot, free for the next chunk's once every wave's products into the hidden layer
@@ -430,19 +475,11 @@ __global__ __launch_bounds__(256 * HW, (GatedShape<P, CP>::OCC)) void k_gated_fw
         if constexpr (P == 1) gated_ahead<0, O::CB * M::KF, AHEAD>();
     }
     if constexpr (HW == 2) {
-        float *const sums = reinterpret_cast<float *>(lds) + wave * (NP * MT * CP) + lane * 4;
         barrier();  // the last operands are read by all
-        if (half == 1)
-#pragma unroll
-            for (int cb = 0; cb < O::CB; ++cb)
-#pragma unroll
-                for (int np = 0; np < NP; ++np)
-#pragma unroll
-                    for (int v = 0; v < NV; v += 4)
-                        *reinterpret_cast<f32x4 *>(sums + ((cb * NP + np) * NV + v) * 64) =
-                            f32x4{acc[cb][np].get(v), acc[cb][np].get(v + 1), acc[cb][np].get(v + 2), acc[cb][np].get(v + 3)};
+        if (half == 1) gated_put_sums<CP, MT, NP>(acc, reinterpret_cast<float *>(lds), wave, lane, NP * MT);
         barrier();
         if (half == 1) return;
+        const float *const sums = reinterpret_cast<float *>(lds) + wave * (NP * MT * CP) + lane * 4;
 #pragma unroll
         for (int cb = 0; cb < O::CB; ++cb)
 #pragma unroll
@@ -454,6 +491,10 @@ __global__ __launch_bounds__(256 * HW, (GatedShape<P, CP>::OCC)) void k_gated_fw
                     for (int t = 0; t < 4; ++t) acc[cb][np].set(v + t, acc[cb][np].get(v + t) + w[t]);
                 }
     }
+    if (S > 1) {
+        gated_put_sums<CP, MT, NP>(acc, part + (split * (int64_t)(gridDim.x / S) + blk) * Sh::PTS * CP, wave, lane, n - p0);
+        return;
+    }
 #pragma unroll
     for (int np = 0; np < NP; ++np) {
         const int64_t p = p0 + np * MT + lane % MT;
@@ -461,36 +502,12 @@ __global__ __launch_bounds__(256 * HW, (GatedShape<P, CP>::OCC)) void k_gated_fw
 #pragma unroll
         for (int cb = 0; cb < O::CB; ++cb) {
             const int c = 32 * cb + NV * (lane / MT);
+            if (c >= C) continue;
             float v[NV];
 #pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] = acc[cb][np].get(i);
-            if (S > 1) store_row<NV>(part + ((int64_t)split * n + p) * CP + c, v);
-            else if (c < C) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i) v[i] += bdp[c + i];
-                store_row<NV>(out + p * C + c, v);
-            }
+            for (int i = 0; i < NV; ++i) v[i] = acc[cb][np].get(i) + bdp[c + i];
+            store_row<NV>(out + p * C + c, v);
         }
-    }
-}
-
-// out[p][c] = b[c] + sum over s of part[s][p][c], in the order of s.  Four channels a thread.
-template <int P, int CP>
-__global__ __launch_bounds__(256) void k_gated_join(const float *__restrict__ part, int64_t n, int C, int S,
-                                                    const float *__restrict__ b, typename GatedIO<P>::T *__restrict__ out) {
-    const int64_t total = n * (C / 4);
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t p = i / (C / 4);
-        const int c = (int)(i % (C / 4)) * 4;
-        f32x4 v = b ? *reinterpret_cast<const f32x4 *>(b + c) : f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-        for (int s = 0; s < S; ++s) {
-            const f32x4 w = *reinterpret_cast<const f32x4 *>(part + ((int64_t)s * n + p) * CP + c);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) v[t] += w[t];
-        }
-#pragma unroll
-        for (int t = 0; t < 4; ++t) out[p * C + c + t] = from_float<typename GatedIO<P>::T>(v[t]);
     }
 }
 
@@ -728,15 +745,19 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
             next(i + 4);
         }
     }
+    if (S > 1) {
+        gated_put_sums<CP, MT, 1>(acc, part + (split * (int64_t)(gridDim.x / S) + blk) * Sh::PTS * CP, wave, lane, n - p0);
+        return;
+    }
     if (!in) return;
 #pragma unroll
     for (int cb = 0; cb < O::CB; ++cb) {
         const int c = 32 * cb + NV * (lane / MT);
+        if (c >= C) continue;
         float v[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) v[i] = acc[cb][0].get(i);
-        if (S > 1) store_row<NV>(part + ((int64_t)split * n + p) * CP + c, v);
-        else if (c < C) store_row<NV>(dx + p * C + c, v);
+        store_row<NV>(dx + p * C + c, v);
     }
 }
 
@@ -840,7 +861,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx_wide(int64_t n, int C, cons
     const int64_t blk = blockIdx.x / S;
     const int split = blockIdx.x % S;
     const int j0 = split * per, j1 = j0 + per < nchunk ? j0 + per : nchunk;
-    const int64_t p = blk * Sh::PTS + wave * 32 + lane % 32;
+    const int64_t p0 = blk * Sh::PTS + wave * 32, p = p0 + lane % 32;
     const uint32_t la = lds_addr(lds);
     auto issue = [&](int j) {
         gated_stage<Sh::B, WAVES>(ops + (size_t)j * O::CHUNK + O::XG, la + (j - j0) % SLOTS * Sh::B, wave, lane);
@@ -883,15 +904,19 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx_wide(int64_t n, int C, cons
     }
     if (j < j1) step(f[0], f[2], j);
     if (j + 1 < j1) step(f[1], f[0], j + 1);
+    if (S > 1) {
+        gated_put_sums<CP, 32, 1>(acc, part + (split * (int64_t)(gridDim.x / S) + blk) * Sh::PTS * CP, wave, lane, n - p0);
+        return;
+    }
     if (p >= n) return;
 #pragma unroll
     for (int cb = 0; cb < O::CB; ++cb) {
         const int c = 32 * cb + 16 * (lane / 32);
+        if (c >= C) continue;
         float v[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) v[i] = acc[cb][0].get(i);
-        if (S > 1) store_row<16>(part + ((int64_t)split * n + p) * CP + c, v);
-        else if (c < C) store_row<16>(dx + p * C + c, v);
+        store_row<16>(dx + p * C + c, v);
     }
 }
 

@@ -12,7 +12,7 @@ struct ts3_gated {
     bool loaded = false;
     unsigned char *ops = nullptr;  // GatedOps
     float *bd = nullptr;           // [CP]
-    float *part = nullptr;         // sums of split outputs [S][n][CP]
+    float *part = nullptr;         // sums of split outputs, a sheet of PTS x CP per workgroup
     void *store = nullptr;         // da, du, h of a tile
     float *wpart = nullptr;        // sums of the weight gradients' splits
     float *bpart = nullptr;        // and of the biases'
@@ -235,8 +235,9 @@ ts3_status ts3_gated_forward(ts3_gated *h, const void *x, int64_t n, void *out, 
             else launch(ic<1>{});
             LAUNCH_CHECK("gated forward");
             if (S > 1) {
-                hipLaunchKernelGGL((k_gated_join<P, CP>), dim3((unsigned)((m * (C / 4) + 255) / 256)), dim3(256), 0, st,
-                                   h->part, m, C, S, h->bd, to);
+                using Sh = GatedShape<P, CP>;
+                hipLaunchKernelGGL((k_gated_join<P, CP, Sh::MT, Sh::NP>), dim3((unsigned)(nb * (Sh::PTS / 4 * CP / 256))),
+                                   dim3(256), 0, st, h->part, m, C, S, (int)nb, h->bd, to);
                 LAUNCH_CHECK("gated join");
             }
         }
@@ -317,8 +318,8 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
             }
             LAUNCH_CHECK("gated dx");
             if (S > 1) {
-                hipLaunchKernelGGL((k_gated_join<P, CP>), dim3((unsigned)((m * (C / 4) + 255) / 256)), dim3(256), 0, st,
-                                   h->part, m, C, S, (const float *)nullptr, dxt);
+                hipLaunchKernelGGL((k_gated_join<P, CP, GatedShape<P, CP>::MT, 1>), dim3((unsigned)(nb * (PTS / 4 * CP / 256))),
+                                   dim3(256), 0, st, h->part, m, C, S, (int)nb, (const float *)nullptr, dxt);
                 LAUNCH_CHECK("gated join");
             }
             const int64_t pps = ((tp + SP - 1) / SP + Dw::KP - 1) / Dw::KP * Dw::KP;
