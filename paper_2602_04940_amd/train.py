@@ -121,9 +121,15 @@ class GatedFeedForward(_Handle):
         L.check(L.lib().ts3_gated_forward(self.h, x.data_ptr(), n, out.data_ptr(), _stream(x)), "ts3_gated_forward")
         return out
 
-    def backward(self, x, g, tile: int = 1 << 18, dx=None):
+    def backward(self, x, g, tile: int | None = None, dx=None):
         """Gradients of sum(g * out) at the loaded weights: (dx, {dWg, dbg, dWu, dbu, dWd, dbd}).
-        forward(x) need not have run; see ts3_gated_backward for `tile`."""
+        forward(x) need not have run.  `tile` points pass at a time, and their da, du and h are
+        kept: by default as many as take 2 GiB (262,144 points at least).  Longer tiles gain up
+        to a tenth at small widths, shorter ones lose: 65,536 points of C = 128, F = 512 in
+        bfloat16 1.07 ms per 500,000 points, 262,144 1.02 ms, 1,048,576 0.93 ms."""
+        if tile is None:
+            row = 3 * ((self.F + 31) // 32 * 32) * x.element_size()
+            tile = max(1 << 18, (1 << 31) // row)
         n = self._rows(x, "x")
         self._rows(g, "g", n)
         if dx is None:
