@@ -1173,52 +1173,57 @@ template <int P, int CP> __global__ __launch_bounds__(256, 2) void k_gated_dw(co
     else gated_dw<P, CP, 0>(A, lds, m, hb, sp);
 }
 
-// The gradients from the splits' sums, in index order: block (hidden tile of 32, channel tile
-// of 32, m), 256 threads.  dWg and dWu are [C][F], dWd [F][C].
+// The gradients from the splits' sums: block (hidden tile of 32, channel tile of 32, m), four
+// groups of 256 threads, each a quarter of the splits in order, then the groups in order.  dWg
+// and dWu are [C][F], dWd [F][C].
 template <int P, int CP>
-__global__ __launch_bounds__(256) void k_gated_grads(const float *__restrict__ part, const float *__restrict__ bpart, int SP,
-                                                     int nchunk, int C, int F, typename GatedIO<P>::T *__restrict__ dWg,
-                                                     typename GatedIO<P>::T *__restrict__ dWu,
-                                                     typename GatedIO<P>::T *__restrict__ dWd,
-                                                     typename GatedIO<P>::T *__restrict__ dbg,
-                                                     typename GatedIO<P>::T *__restrict__ dbu,
-                                                     typename GatedIO<P>::T *__restrict__ dbd) {
+__global__ __launch_bounds__(1024) void k_gated_grads(const float *__restrict__ part, const float *__restrict__ bpart, int SP,
+                                                      int nchunk, int C, int F, typename GatedIO<P>::T *__restrict__ dWg,
+                                                      typename GatedIO<P>::T *__restrict__ dWu,
+                                                      typename GatedIO<P>::T *__restrict__ dWd,
+                                                      typename GatedIO<P>::T *__restrict__ dbg,
+                                                      typename GatedIO<P>::T *__restrict__ dbu,
+                                                      typename GatedIO<P>::T *__restrict__ dbd) {
     using T = typename GatedIO<P>::T;
-    __shared__ float tile[32][33];
+    constexpr int GROUPS = 4;
+    __shared__ double sums[GROUPS][32][33];
     const int ht = blockIdx.x, ct = blockIdx.y, m = blockIdx.z;
     const int FP = nchunk * 32, BW = FP > CP ? FP : CP;
-    const int col = threadIdx.x & 31, r8 = threadIdx.x >> 5;
+    const int q = threadIdx.x >> 8, col = threadIdx.x & 31, r8 = (threadIdx.x >> 5) & 7;
+    const int per = (SP + GROUPS - 1) / GROUPS, s0 = q * per, s1 = s0 + per < SP ? s0 + per : SP;
     const int64_t stride = (int64_t)3 * FP * CP;
     double v[4] = {0.0, 0.0, 0.0, 0.0};
     const float *src = part + ((int64_t)m * FP + 32 * ht + r8) * CP + 32 * ct + col;
 #pragma unroll 8
-    for (int s = 0; s < SP; ++s)
+    for (int s = s0; s < s1; ++s)
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] += src[s * stride + (int64_t)8 * i * CP];
-    if (m == 2) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int f = 32 * ht + r8 + 8 * i, c = 32 * ct + col;
-            if (f < F && c < C) dWd[(int64_t)f * C + c] = from_float<T>((float)v[i]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tile[r8 + 8 * i][col] = (float)v[i];
-        __syncthreads();
-        T *const to = m ? dWu : dWg;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int f = 32 * ht + col, c = 32 * ct + r8 + 8 * i;
-            if (f < F && c < C) to[(int64_t)c * F + f] = from_float<T>(tile[col][r8 + 8 * i]);
-        }
-    }
+    for (int i = 0; i < 4; ++i) sums[q][r8 + 8 * i][col] = v[i];
     // Column sums: by the first channel tile's blocks (da, du), the first hidden tile's (g).
-    if (threadIdx.x < 32 && (m == 2 ? ht == 0 : ct == 0)) {
-        const int at = 32 * (m == 2 ? ct : ht) + col;
+    const bool columns = m == 2 ? ht == 0 : ct == 0;
+    const int at = 32 * (m == 2 ? ct : ht) + col;
+    if (columns && r8 == 0) {
         double s = 0.0;
-        for (int i = 0; i < SP; ++i) s += bpart[((int64_t)i * 3 + m) * BW + at];
-        T *const to = m == 0 ? dbg : m == 1 ? dbu : dbd;
-        if (at < (m == 2 ? C : F)) to[at] = from_float<T>((float)s);
+#pragma unroll 8
+        for (int i = s0; i < s1; ++i) s += bpart[((int64_t)i * 3 + m) * BW + at];
+        sums[q][col][32] = s;
+    }
+    __syncthreads();
+    const int a = threadIdx.x >> 5, b = threadIdx.x & 31;  // one value a thread, b along the gradient's rows
+    const int f = 32 * ht + (m == 2 ? a : b), c = 32 * ct + (m == 2 ? b : a);
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) sum += m == 2 ? sums[i][a][b] : sums[i][b][a];
+    if (f < F && c < C) {
+        if (m == 2) dWd[(int64_t)f * C + c] = from_float<T>((float)sum);
+        else (m ? dWu : dWg)[(int64_t)c * F + f] = from_float<T>((float)sum);
+    }
+    if (columns && threadIdx.x < 32 && at < (m == 2 ? C : F)) {
+        double s = 0.0;
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) s += sums[i][col][32];
+        (m == 0 ? dbg : m == 1 ? dbu : dbd)[at] = from_float<T>((float)s);
     }
 }
 
