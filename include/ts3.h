@@ -413,7 +413,8 @@ ts3_status ts3_gated_forward(ts3_gated *h, const void *x, int64_t n, void *out, 
  * (which need not have run: the hidden layer is recomputed).  dx [n, C]
  * (neither x nor g) and the weight gradients.  The points pass in tiles of `tile`
  * (at most 2^24 are taken): a tile's da, du and h stay in a store of
- * 3 F min(tile, n) elements between the two kernels that make and use them.
+ * 3 F min(tile, n) elements (in bfloat16 1/24 more, for sums of da and du as they
+ * are before their rounding) between the kernels that make and use them.
  * The store is allocated by the first call, or a later one that needs more
  * (this synchronises; TS3_ERR_OUT_OF_MEMORY if it does not fit), and kept.
  * Sums over points are in a fixed order for given n and tile.  n == 0 writes

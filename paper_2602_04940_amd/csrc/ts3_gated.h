@@ -14,6 +14,7 @@
 //   k_gated_join   sums of outputs whose hidden units were split over workgroups
 //   k_gated_dx     recomputes the hidden layer, gives dx, and leaves da, du and h of a
 //                  tile of points in the store
+//   k_gated_slopes, k_gated_dx_wide   the same in two kernels, for wide bfloat16 points
 //   k_gated_dw     the three weight gradients of the tile: products over its points
 //   k_gated_grads  sums over the splits of the points, in index order
 //
@@ -110,9 +111,11 @@ enum { GATED_SILU = 0, GATED_GELU = 1 };
 // The bfloat16 backward takes Phi by Abramowitz & Stegun 7.1.26: a polynomial in t = 1 / (1 +
 // p |z|) times e^(-z^2), z = a / sqrt 2, whose exponential is also the density's; within 7.5e-8 of
 // Phi, which the slope needs where it crosses zero (a = -0.75).  The bfloat16 forward takes
-// Phi(a) ~ 1 / (1 + 2^-u), u = a (K1 + K2 a^2 + K3 a^4), the K fitted here (minimax over
-// [-12, 12]): within 8.1e-5 of GELU, where bfloat16 rounds a hidden value of one by 2e-3, with 6 of
-// 17 instructions less.  a^2 stops at 60, past which Phi is 0 or 1 and K3 would turn u round.
+// Phi(a) ~ 1 / (1 + 2^-u), u = a (K1 + K2 a^2 + K3 a^4 + K4 a^6), the K fitted here (minimax of
+// the error over |GELU| + 1e-6 on [-13, 13]): within 1.2e-3 of GELU, also where it vanishes, less
+// than a bfloat16 rounding of the hidden value (2e-3), with 5 of 17 instructions less.  Three K
+// are within 8e-5 but lose 13% of GELU(-4).  a^2 stops at 42, past which
+// Phi is 0 or 1.
 template <int P, int ACT, bool SLOPE> __device__ __forceinline__ float gated_act(float a, float &slope) {
     constexpr float LOG2E = 1.44269504f;
     if constexpr (ACT == GATED_SILU) {
@@ -121,9 +124,9 @@ template <int P, int ACT, bool SLOPE> __device__ __forceinline__ float gated_act
         if (SLOPE) slope = s + (y - y * s);
         return y;
     } else if constexpr (P == 1 && !SLOPE) {
-        constexpr float K1 = 2.30340187f, K2 = 0.104987341f, K3 = -7.60263942e-4f;
-        const float a2 = fminf(a * a, 60.f);
-        return a * fast_rcp(1.f + fast_exp2(a * (-K1 + a2 * (-K2 + a2 * -K3))));
+        constexpr float K1 = 2.29720153f, K2 = 0.109516947f, K3 = -1.43191115e-3f, K4 = 1.3191713e-5f;
+        const float a2 = fminf(a * a, 42.f);
+        return a * fast_rcp(1.f + fast_exp2(a * (-K1 - a2 * (K2 + a2 * (K3 + a2 * K4)))));
     } else {
         float phi, e = 0.f;
         if (SLOPE) e = fast_exp2((-0.5f * LOG2E) * (a * a));
@@ -519,14 +522,45 @@ __global__ __launch_bounds__(256 * HW, (GatedShape<P, CP>::OCC)) void k_gated_fw
     }
 }
 
+// Sums over the 32 points (lanes 0..31 and 32..63) of 16 values of da and du each, as they are
+// before bfloat16 rounds them: summed as the store holds them, every point's rounding stays in
+// dbg and dbu (1.6 times the error of the output's own rounding, measured at 50 to 500 points).
+// Each step adds two lanes and merges two values into the halves that this frees, so the 32
+// values take 77 instructions instead of 160: add() leaves value i of da in the lower and of du
+// in the upper row of 16, store() merges the 16 that are left.  Lane l ends with value l & 15 of
+// its half, of du if l & 16.
+struct GatedColumns {
+    float r[16];
+    __device__ __forceinline__ void add(int v, float da, float du) {
+        auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(da), __float_as_uint(du), false, false);
+        r[v] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    template <int CTRL, int N> __device__ __forceinline__ void merge(int lane) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float a = r[i] + dpp<CTRL>(r[i]), b = r[i + N] + dpp<CTRL>(r[i + N]);
+            r[i] = lane & N ? b : a;
+        }
+    }
+    // To row w of chunk j: cols[m][chunk][rows][32], m = 0 da, 1 du.
+    __device__ __forceinline__ void store(float *cols, int nchunk, int j, int64_t rows, int64_t w, int lane) {
+        merge<0x128, 8>(lane);  // row_ror:8
+        merge<0x141, 4>(lane);  // row_half_mirror
+        merge<0x4E, 2>(lane);   // quad_perm [2,3,0,1]
+        merge<0xB1, 1>(lane);   // quad_perm [1,0,3,2]
+        const int m = (lane >> 4) & 1;
+        cols[(((int64_t)m * nchunk + j) * rows + w) * 32 + 16 * (lane >> 5) + (lane & 15)] = r[0];
+    }
+};
+
 // The hidden layer of a chunk before the activation, and the gradient of its output.
 template <int MT> struct GatedHidden {
     Rows32<MT> a[1], u[1], dh[1];
 };
 
 // dx of n points (the first nb * PTS of the store's rows), and da, du, h in the store:
-// store[m][chunk][tp][32], m = 0 da, 1 du, 2 h; rows of points past n are zero.  Grid and
-// splits as k_gated_fwd.
+// store[m][chunk][tp][32], m = 0 da, 1 du, 2 h; rows of points past n are zero.  In bfloat16 also
+// the sums of da and du over 32 points each, in cols (GatedColumns).  Grid and splits as k_gated_fwd.
 // A wave's rows and sums fill half of its registers or more, so one or two waves share a
 // SIMD, and one wave alone issues its vector work beside its own products or not at all: the
 // products into the hidden layer of chunk j + 1 are interleaved with the slopes of chunk j,
@@ -536,7 +570,8 @@ template <int P, int CP, int ACT>
 __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
     const typename GatedIO<P>::T *__restrict__ x, const typename GatedIO<P>::T *__restrict__ g, int64_t n, int C,
     const unsigned char *__restrict__ ops, int nchunk, int per, int S, int64_t tp,
-    typename GatedIO<P>::T *__restrict__ store, typename GatedIO<P>::T *__restrict__ dx, float *__restrict__ part) {
+    typename GatedIO<P>::T *__restrict__ store, float *__restrict__ cols, typename GatedIO<P>::T *__restrict__ dx,
+    float *__restrict__ part) {
     using T = typename GatedIO<P>::T;
     using Sh = GatedShapeX<P, CP>;
     constexpr int MT = Sh::MT, WAVES = Sh::WAVES;
@@ -544,7 +579,7 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
     using O = GatedOps<P, CP, MT>;
     constexpr int NV = M::NV, KS = O::KS;
     // Stores of a chunk: they are issued after its copies and may stay in flight while those are waited for.
-    constexpr int STORES = 3 * NV * (int)sizeof(T) / 16;
+    constexpr int STORES = 3 * NV * (int)sizeof(T) / 16 + (P == 1);
     __shared__ __attribute__((aligned(1024))) unsigned char lds[Sh::LDS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int64_t blk = blockIdx.x / S;
@@ -595,6 +630,7 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
     // da, du and h of values v0 .. v1 - 1 of chunk j; each eight, as they are complete, become
     // the next products' operands and 16 or 32 bytes of the store's rows.
     float da[8], du[8], h[8];
+    GatedColumns sums;
     auto slopes = [&](GatedHidden<MT> &c, int j, int v0, int v1) {
 #pragma unroll
         for (int v = v0; v < v1; ++v) {
@@ -604,6 +640,7 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
             h[v & 7] = in ? y * uv : 0.f;
             du[v & 7] = d * y;
             da[v & 7] = d * uv * slope;
+            if constexpr (P == 1) sums.add(v, da[v & 7], du[v & 7]);
             if ((v & 7) == 7) {
                 to_parts(da, daf[0][v >> 3]);
                 to_parts(du, duf[0][v >> 3]);
@@ -614,6 +651,8 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
                 store_row<8>(row + 2 * plane, h);
             }
         }
+        if constexpr (P == 1)
+            if (v1 == NV) sums.store(cols, nchunk, j, tp / 32, p0 / 32, lane);
     };
     auto barrier = [&]() {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -778,13 +817,13 @@ template <int CP> struct GatedWide {
     static constexpr int A = 1024 + 3 * CP * 64, B = 2 * CP * 64;
 };
 
-// da, du and h of chunks per*s .. of PTS points, as k_gated_dx leaves them in the store.  One LDS
+// da, du, h and cols of chunks per*s .. of PTS points, as k_gated_dx leaves them.  One LDS
 // slot: the next chunk is copied while the slopes of this one are computed.
 template <int CP, int ACT>
 __global__ __launch_bounds__(256, 2) void k_gated_slopes(const bf16_t *__restrict__ x, const bf16_t *__restrict__ g,
                                                          int64_t n, int C, const unsigned char *__restrict__ ops,
                                                          int nchunk, int per, int S, int64_t tp,
-                                                         bf16_t *__restrict__ store) {
+                                                         bf16_t *__restrict__ store, float *__restrict__ cols) {
     using Sh = GatedWide<CP>;
     using O = GatedOps<1, CP, 32>;
     constexpr int WAVES = Sh::WAVES, KS = O::KS;
@@ -811,6 +850,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_slopes(const bf16_t *__restric
     auto slopes = [&](int j) {
         asm volatile("" ::: "memory");
         bf16_t *const row = store + ((int64_t)j * tp + p) * 32 + 16 * (lane / 32);
+        GatedColumns sums;
 #pragma unroll
         for (int v0 = 0; v0 < 16; v0 += 8) {
             float da[8], du[8], h[8];
@@ -822,17 +862,19 @@ __global__ __launch_bounds__(256, 2) void k_gated_slopes(const bf16_t *__restric
                 h[v] = in ? y * uv : 0.f;
                 du[v] = d * y;
                 da[v] = d * uv * slope;
+                sums.add(v0 + v, da[v], du[v]);
             }
             store_row<8>(row + v0, da);
             store_row<8>(row + plane + v0, du);
             store_row<8>(row + 2 * plane + v0, h);
         }
+        sums.store(cols, nchunk, j, tp / 32, p0 / 32, lane);
         asm volatile("" ::: "memory");
     };
 #pragma unroll 1
     for (int j = j0; j < j1; ++j) {
-        // The copies of chunk j are older than the six stores of chunk j - 1.
-        if (j > j0) wait_vmcnt<6>();
+        // The copies of chunk j are older than the seven stores of chunk j - 1.
+        if (j > j0) wait_vmcnt<7>();
         else wait_vmcnt<0>();
         barrier();  // chunk j is in LDS
         const unsigned char *const sec = lds + 1024;
@@ -969,9 +1011,11 @@ __device__ __forceinline__ float sum_slots(const bf16x8 &v, float s) {
 // `zeros` (16 bytes).
 // SUMS: column sums that the workgroup takes as it reads its operands, of the hidden columns
 // (1), of the channels (2) or none (0).  Every wave takes them, wanted or not: beside the
-// products they are free, branches around them are not.
+// products they are free, branches around them are not.  In bfloat16 those of the hidden
+// columns come from cols instead, after the products.
 template <int P, int CP> struct GatedDwArgs {
     const typename GatedIO<P>::T *x, *g, *store;
+    const float *cols;
     int64_t n, tp, per;
     int C, nchunk, nhb, first;
     const unsigned char *zeros;
@@ -1027,7 +1071,7 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
     };
     f32x16 acc[2][CTW];
     double bsum[2] = {0.0, 0.0}, gsum[CTW];
-    const bool bh = SUMS == 1 && ci == 0, bc = SUMS == 2 && hi == 0;
+    const bool bh = P == 3 && SUMS == 1 && ci == 0, bc = SUMS == 2 && hi == 0;
     float *const bp = A.bpart + ((int64_t)sp * 3 + m) * BW;
     float *const wp = A.part + (((int64_t)sp * 3 + m) * FP + hb * S::HB + hi * 64) * CP + ci * CTW * 32;
     auto hidden_in = [&](int t) { return hb * S::HB + hi * 64 + t * 32 < FP; };
@@ -1053,7 +1097,7 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
                     af[t].p[p] = plane_tr(slot + ((2 * hi + t) * P + p) * S::PLB, r0, lane);
-                    if constexpr (SUMS == 1) bs[t] = sum_slots(af[t].p[p], bs[t]);
+                    if constexpr (P == 3 && SUMS == 1) bs[t] = sum_slots(af[t].p[p], bs[t]);
                 }
 #pragma unroll
             for (int c = 0; c < CTW; ++c) {
@@ -1160,6 +1204,31 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
             const float s = (float)(bsum[t] + __shfl_xor(bsum[t], 32));
             float *const to = bp + hb * S::HB + hi * 64 + t * 32 + (lane & 31);
             if (lane < 32) *to = first ? s : *to + s;
+        }
+    }
+    if constexpr (P == 1 && SUMS == 1) {
+        // Rows of 32 points and chunks of the split: eight lanes a row, TPC a chunk.
+        static_assert(KP == 32, "a split is whole rows of cols");
+        constexpr int TPC = 256 / HPL;
+        const int ch = hb * HPL + threadIdx.x / TPC, row = threadIdx.x % TPC / 8, c4 = 4 * (threadIdx.x & 7);
+        if (ch < nchunk) {
+            const float *const src = A.cols + (((int64_t)m * nchunk + ch) * (tp / 32) + a0 / 32) * 32 + c4;
+            double s[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 8
+            for (int k = row; k < nk; k += TPC / 8) {
+                const f32x4 v = *reinterpret_cast<const f32x4 *>(src + (int64_t)k * 32);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] += v[i];
+            }
+#pragma unroll
+            for (int x = 8; x < TPC; x <<= 1)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] += __shfl_xor(s[i], x);
+            if (row == 0) {
+                float *const to = bp + ch * 32 + c4;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) to[i] = first ? (float)s[i] : (float)(to[i] + s[i]);
+            }
         }
     }
     if (bc)

@@ -278,7 +278,9 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
         const int64_t step = std::min(std::min(tile, GATED_TILE_MAX), std::max<int64_t>(n, 1));
         const int SP = n > 0 ? gated_point_splits<P, CP>(nchunk, step) : 0;
         if (n > 0) {
-            const int64_t need = (step + PTS - 1) / PTS * PTS * 3 * FP * (int64_t)sizeof(T);
+            // da, du and h of a tile, and in bfloat16 the sums of da and du over 32 points each
+            const int64_t rows = (step + PTS - 1) / PTS * PTS;
+            const int64_t need = rows * 3 * FP * (int64_t)sizeof(T) + (P == 1 ? rows / 32 * 2 * FP * 4 : 0);
             const int most = gated_point_splits<P, CP>(nchunk, GATED_TILE_MAX);
             const int64_t wbytes = (int64_t)most * 3 * FP * CP * 4, bbytes = (int64_t)most * 3 * BW * 4;
             if (!h->wpart) {
@@ -309,17 +311,18 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
             const T *const xt = (const T *)x + t0 * C, *const gt = (const T *)g + t0 * C;
             T *const dxt = (T *)dx + t0 * C;
             const bool silu = h->desc.activation == TS3_SILU;
+            float *const cols = P == 1 ? (float *)((T *)h->store + tp * 3 * FP) : nullptr;
             if constexpr (WIDE) {
                 const auto slopes = silu ? &k_gated_slopes<CP, GATED_SILU> : &k_gated_slopes<CP, GATED_GELU>;
                 hipLaunchKernelGGL(slopes, dim3((unsigned)(nb * S)), dim3(256), 0, st, xt, gt, m, C, h->ops, nchunk, per,
-                                   S, tp, (T *)h->store);
+                                   S, tp, (T *)h->store, cols);
                 LAUNCH_CHECK("gated slopes");
                 hipLaunchKernelGGL(k_gated_dx_wide<CP>, dim3((unsigned)(nb * S)), dim3(256), 0, st, m, C, h->ops, nchunk,
                                    per, S, tp, (const T *)h->store, dxt, h->part);
             } else {
                 const auto kernel = silu ? &k_gated_dx<P, CP, GATED_SILU> : &k_gated_dx<P, CP, GATED_GELU>;
                 hipLaunchKernelGGL(kernel, dim3((unsigned)(nb * S)), dim3(256), 0, st, xt, gt, m, C, h->ops, nchunk, per,
-                                   S, tp, (T *)h->store, dxt, h->part);
+                                   S, tp, (T *)h->store, cols, dxt, h->part);
             }
             LAUNCH_CHECK("gated dx");
             if (S > 1) {
@@ -328,7 +331,7 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
                 LAUNCH_CHECK("gated join");
             }
             const int64_t pps = ((tp + SP - 1) / SP + Dw::KP - 1) / Dw::KP * Dw::KP;
-            const GatedDwArgs<P, CP> a{xt, gt, (const T *)h->store, m, tp, pps, C, nchunk, nhb, t0 == 0, zeros, h->wpart,
+            const GatedDwArgs<P, CP> a{xt, gt, (const T *)h->store, cols, m, tp, pps, C, nchunk, nhb, t0 == 0, zeros, h->wpart,
                                        h->bpart};
             hipLaunchKernelGGL((k_gated_dw<P, CP>), dim3((unsigned)(3 * nhb * SP)), dim3(256), 0, st, a);
             LAUNCH_CHECK("gated weight gradients");

@@ -105,6 +105,10 @@ class GatedFeedForward(_Handle):
         L.check(L.lib().ts3_gated_bytes(self.h, ct.byref(b)), "ts3_gated_bytes")
         return b.value
 
+    def default_tile(self) -> int:
+        row = 3 * ((self.F + 31) // 32 * 32) * (2 if self.torch_dtype is torch.bfloat16 else 4)
+        return max(min(1 << 18, (1 << 33) // row), (1 << 31) // row)
+
     def load(self, w: GatedWeights):
         if (w.C, w.F, w.torch_dtype) != (self.C, self.F, self.torch_dtype):
             raise ValueError(f"weights of C={w.C}, F={w.F}, {w.torch_dtype} for an operator of C={self.C}, F={self.F}, "
@@ -124,12 +128,12 @@ class GatedFeedForward(_Handle):
     def backward(self, x, g, tile: int | None = None, dx=None):
         """Gradients of sum(g * out) at the loaded weights: (dx, {dWg, dbg, dWu, dbu, dWd, dbd}).
         forward(x) need not have run.  `tile` points pass at a time, and their da, du and h are
-        kept: by default as many as take 2 GiB (262,144 points at least).  Longer tiles gain up
-        to a tenth at small widths, shorter ones lose: 65,536 points of C = 128, F = 512 in
-        bfloat16 1.07 ms per 500,000 points, 262,144 1.02 ms, 1,048,576 0.93 ms."""
+        kept: by default as many as take 2 GiB, 262,144 at least if those take no more than 8.
+        Longer tiles gain up to a tenth at small widths, shorter ones lose: 65,536 points of
+        C = 128, F = 512 in bfloat16 1.07 ms per 500,000 points, 262,144 1.02 ms, 1,048,576
+        0.93 ms."""
         if tile is None:
-            row = 3 * ((self.F + 31) // 32 * 32) * x.element_size()
-            tile = max(1 << 18, (1 << 31) // row)
+            tile = self.default_tile()
         n = self._rows(x, "x")
         self._rows(g, "g", n)
         if dx is None:

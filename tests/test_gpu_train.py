@@ -136,6 +136,41 @@ def test_gated_gates_far_from_zero(kind, dtype):
         _check(n, grads[n], ref[n], dtype, (C, F, N))
 
 
+# Padded widths of every kernel, one point to several tiles, hidden widths around a chunk.
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+@pytest.mark.parametrize("N,C,F,tile", [(1, 64, 32, 1000), (70, 48, 33, 64), (3001, 128, 300, 1024), (300, 192, 31, 1000),
+                                        (5003, 256, 100, 2048)])
+def test_gated_bf16_bias_gradients_round_once(N, C, F, tile, kind):
+    """dbg, dbu and dbd are sums of float32 values, rounded to bfloat16 once: within 2^-8 of each
+    value, plus what float32 sums and exponentials good to some 2^-21 leave of the largest."""
+    import torch
+    from oracle import train as T
+    x, w, g = _gated(N, C, F, "bf16", True, seed=6)
+    with _operator(C, F, kind, "bf16", w) as ff:
+        _, grads = ff.backward(to_device(x, "bf16"), to_device(g, "bf16"), tile=tile)
+        torch.cuda.synchronize()
+    ref = T.gated_backward(x, w, kind, g)
+    for n in ("dbg", "dbu", "dbd"):
+        err = np.abs(to_host(grads[n]) - ref[n])
+        assert (err <= 2.0 ** -8 * np.abs(ref[n]) + 2.0 ** -16 * np.abs(ref[n]).max()).all(), n
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+@pytest.mark.parametrize("gate", [-3.0, -4.0, -5.0])
+def test_gated_gates_that_are_nearly_closed(gate, kind, dtype):
+    """Every gate far down its tail: the outputs are small, and as exact relative to themselves."""
+    import torch
+    from oracle import train as T
+    N, C, F = 200, 96, 70
+    x, w, _ = _gated(N, C, F, dtype, True, seed=7, scale=0.05)
+    w["bg"], w["bd"] = np.full(F, gate), np.zeros(C)
+    with _operator(C, F, kind, dtype, w) as ff:
+        out = ff.forward(to_device(x, dtype))
+        torch.cuda.synchronize()
+    _check("out", out, T.gated_forward(x, w, kind), dtype, (C, F))
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("N", [5, 300, 50_000])
 def test_gated_rows_are_independent(N, dtype):

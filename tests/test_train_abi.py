@@ -86,3 +86,14 @@ def test_tensor_tables_are_refused_before_any_device_call():
                               (None, None, TypeError), ([], 5, TypeError)):
         with pytest.raises(error):
             _tensors.clip_table(grads, out)
+
+
+@pytest.mark.parametrize("F", [1, 24, 512, 1024, 5000, 65536])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_default_tile_bounds_the_store(F, dtype):
+    from paper_2602_04940_amd import GatedFeedForward
+    ff = GatedFeedForward.__new__(GatedFeedForward)
+    ff.F, ff.torch_dtype = F, dtype
+    tile, row = ff.default_tile(), 3 * ((F + 31) // 32 * 32) * (2 if dtype is torch.bfloat16 else 4)
+    assert tile >= 8192 and tile * row <= 1 << 33
+    assert tile >= 1 << 18 or F >= 2048
