@@ -14,7 +14,8 @@
 //   k_gated_join   sums of outputs whose hidden units were split over workgroups
 //   k_gated_dx     recomputes the hidden layer, gives dx, and leaves da, du and h of a
 //                  tile of points in the store
-//   k_gated_slopes, k_gated_dx_wide   the same in two kernels, for wide bfloat16 points
+//   k_gated_slopes, k_gated_slopes3, k_gated_dx_wide   the same in two kernels, for bfloat16 points
+//                  wider than 128 and float32 ones of 65 to 128 channels
 //   k_gated_dw     the three weight gradients of the tile: products over its points
 //   k_gated_grads  sums over the splits of the points, in index order
 //
@@ -80,7 +81,34 @@ __device__ __forceinline__ void to_parts(const float (&v)[8], Parts<1> &f) {
 }
 __device__ __forceinline__ void to_parts(const float (&v)[8], Parts<3> &f) { split8(v, f); }
 
-// d += a b, the part products smallest first.
+// d[i] += a[i] b[i] for N results in turn, the part products smallest first: a product that adds
+// to the one before it takes twice as long.
+// `beside(q)` is issued after part product q of each.
+template <int MT, int P, int N, typename F>
+__device__ __forceinline__ void mma_parts_in_turn(typename Mat<MT>::D *const (&d)[N], const Parts<P> (&a)[N],
+                                                  const Parts<P> *const (&b)[N], F beside) {
+    using PP = PartProducts<P, P>;
+#pragma unroll
+    for (int q = 0; q < PP::N; ++q) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) Mat<MT>::mma(*d[i], a[i].p[PP::I[q]], b[i]->p[PP::J[q]]);
+        beside(q);
+        // The compiler would put each result's products back into a row, and what goes beside them
+        // before them: only loads, stores and scalar instructions may pass here.
+        if constexpr (P > 1) __builtin_amdgcn_sched_barrier(0x094);
+    }
+}
+template <int MT, int P, int N>
+__device__ __forceinline__ void mma_parts_in_turn(typename Mat<MT>::D *const (&d)[N], const Parts<P> (&a)[N],
+                                                  const Parts<P> *const (&b)[N]) {
+    using PP = PartProducts<P, P>;
+#pragma unroll
+    for (int q = 0; q < PP::N; ++q) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) Mat<MT>::mma(*d[i], a[i].p[PP::I[q]], b[i]->p[PP::J[q]]);
+        if constexpr (P > 1) __builtin_amdgcn_sched_barrier(0x096);
+    }
+}
 template <int MT, int P>
 __device__ __forceinline__ void mma_parts(typename Mat<MT>::D &d, const Parts<P> &a, const Parts<P> &b) {
     using PP = PartProducts<P, P>;
@@ -298,13 +326,15 @@ __device__ __forceinline__ void gated_channels(const unsigned char *sec, const P
 #pragma unroll
     for (int s = 0; s < M::KF; ++s)
 #pragma unroll
-        for (int cb = 0; cb < CP / 32; ++cb)
+        for (int cb = 0; cb < CP / 32; cb += 2)
 #pragma unroll
             for (int t = 0; t < M::HT; ++t) {
-                Parts<P> a;
-                lds_parts(sec, (cb * M::HT + t) * M::KF + s, lane, a);
+                Parts<P> a[2];
 #pragma unroll
-                for (int np = 0; np < NP; ++np) mma_parts<MT, P>(acc[cb][np].d[t], a, hf[np][s]);
+                for (int i = 0; i < 2; ++i) lds_parts(sec, ((cb + i) * M::HT + t) * M::KF + s, lane, a[i]);
+#pragma unroll
+                for (int np = 0; np < NP; ++np)
+                    mma_parts_in_turn<MT, P, 2>({&acc[cb][np].d[t], &acc[cb + 1][np].d[t]}, a, {&hf[np][s], &hf[np][s]});
             }
 }
 // Order of a region of N products that read one operand each from LDS (P = 1), and PRE reads
@@ -342,7 +372,7 @@ template <int P, int CP> struct GatedShape {
 };
 template <int P, int CP> struct GatedShapeX {
     static constexpr int MT = GatedShape<P, CP>::MT, WAVES = 4, PTS = WAVES * MT;
-    static constexpr int OCC = P == 1 && CP <= 128 ? 2 : P == 3 && CP <= 64 ? 2 : 1;
+    static constexpr int OCC = P == 3 && CP > 64 ? 1 : 2;
     static constexpr int LDS_MAX = 160 * 1024 / OCC, A = 1024 + 3 * CP * 64 * P, B = 2 * CP * 64 * P;
     // Where the five sections of a chunk do not fit LDS, they pass one by one through three slots.
     static constexpr bool RING = A + B > LDS_MAX;
@@ -464,10 +494,16 @@ __global__ __launch_bounds__(256 * HW, (GatedShape<P, CP>::OCC)) void k_gated_fw
         gated_bias<MT, NP>(sa, 0, lane, a);
         gated_bias<MT, NP>(sa, 1, lane, u);
 #pragma unroll
-        for (int ks = 0; ks < O::KS; ++ks) {  // in turn: a product that adds to the one before it takes twice as long
-            gated_hidden<P, CP, MT, NP>(sa + 1024, xf, ks, lane, a);
-            gated_hidden<P, CP, MT, NP>(sa + 1024 + O::SEC, xf, ks, lane, u);
-        }
+        for (int ks = 0; ks < O::KS; ++ks)
+#pragma unroll
+            for (int t = 0; t < M::HT; ++t) {
+                Parts<P> w[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) lds_parts(sa + 1024 + k * O::SEC, t * O::KS + ks, lane, w[k]);
+#pragma unroll
+                for (int np = 0; np < NP; ++np)
+                    mma_parts_in_turn<MT, P, 2>({&a[np].d[t], &u[np].d[t]}, w, {&xf[np][ks], &xf[np][ks]});
+            }
         if constexpr (P == 1) gated_ahead<8, 2 * O::KS, AHEAD>();
         if (DSLOTS == 1) wait_vmcnt<0>();
         barrier();  // (G, U) of chunk i are read by all; with one slot, D is in LDS
@@ -553,19 +589,31 @@ struct GatedColumns {
     }
 };
 
+// The store holds da, du and h (m = 0, 1, 2) by chunks and blocks of 32 points, each as the lanes
+// of a 32 x 32 result hold it, 16 bytes of every lane after another: store[m][chunk][tp / 32][1024],
+// so that a wave writes and reads whole lines.  (By rows of 32 hidden units, 16 bytes of a lane to
+// a row, the requests bound every kernel that touches it: STORE_GAIN.)
+// Place in its block of hidden unit h (a multiple of the 16 bytes' values) of point p.
+template <int P> __host__ __device__ constexpr int gated_at(int p, int h) {
+    constexpr int V = P == 1 ? 8 : 4;
+    return (h % 16 / V * 64 + h / 16 * 32 + p) * V;
+}
+// Eight values of a lane at their place.
+__device__ __forceinline__ void gated_put(bf16_t *at, const float (&v)[8]) { store_row<8>(at, v); }
+__device__ __forceinline__ void gated_put(float *at, const float (&v)[8]) {
+    *reinterpret_cast<f32x4 *>(at) = f32x4{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4 *>(at + 256) = f32x4{v[4], v[5], v[6], v[7]};
+}
+
 // The hidden layer of a chunk before the activation, and the gradient of its output.
 template <int MT> struct GatedHidden {
     Rows32<MT> a[1], u[1], dh[1];
 };
 
-// dx of n points (the first nb * PTS of the store's rows), and da, du, h in the store:
-// store[m][chunk][tp][32], m = 0 da, 1 du, 2 h; rows of points past n are zero.  In bfloat16 also
+// dx of n points (the first nb * PTS of the store's), and da, du, h in the store; values of points past n are zero.  In bfloat16 also
 // the sums of da and du over 32 points each, in cols (GatedColumns).  Grid and splits as k_gated_fwd.
-// A wave's rows and sums fill half of its registers or more, so one or two waves share a
-// SIMD, and one wave alone issues its vector work beside its own products or not at all: the
-// products into the hidden layer of chunk j + 1 are interleaved with the slopes of chunk j,
-// some values after each K step, followed by chunk j's products into dx.  (G, U, H) have two
-// LDS slots where they fit, else one, (XG, XU) have one; copies are issued a phase ahead.
+// (G, U, H) have two LDS slots where they fit, else one, (XG, XU) have one; copies are issued a
+// phase ahead.
 template <int P, int CP, int ACT>
 __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
     const typename GatedIO<P>::T *__restrict__ x, const typename GatedIO<P>::T *__restrict__ g, int64_t n, int C,
@@ -618,13 +666,10 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
     auto hidden = [&](GatedHidden<MT> &c, const unsigned char *sec, int ks) {
 #pragma unroll
         for (int t = 0; t < M::HT; ++t) {
-            Parts<P> wg, wu, wd;
-            lds_parts(sec, t * KS + ks, lane, wg);
-            lds_parts(sec + O::SEC, t * KS + ks, lane, wu);
-            lds_parts(sec + 2 * O::SEC, t * KS + ks, lane, wd);
-            mma_parts<MT, P>(c.a[0].d[t], wg, xf[0][ks]);
-            mma_parts<MT, P>(c.u[0].d[t], wu, xf[0][ks]);
-            mma_parts<MT, P>(c.dh[0].d[t], wd, gf[0][ks]);
+            Parts<P> w[3];
+#pragma unroll
+            for (int i = 0; i < 3; ++i) lds_parts(sec + i * O::SEC, t * KS + ks, lane, w[i]);
+            mma_parts_in_turn<MT, P, 3>({&c.a[0].d[t], &c.u[0].d[t], &c.dh[0].d[t]}, w, {&xf[0][ks], &xf[0][ks], &gf[0][ks]});
         }
     };
     // da, du and h of values v0 .. v1 - 1 of chunk j; each eight, as they are complete, become
@@ -644,11 +689,11 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
             if ((v & 7) == 7) {
                 to_parts(da, daf[0][v >> 3]);
                 to_parts(du, duf[0][v >> 3]);
-                T *const row = store + ((int64_t)j * tp + p) * 32 + NV * (lane / MT) + (v & ~7);
+                T *const at = store + ((int64_t)j * tp + p / 32 * 32) * 32 + gated_at<P>(p % 32, NV * (lane / MT) + (v & ~7));
                 const int64_t plane = (int64_t)nchunk * tp * 32;
-                store_row<8>(row, da);
-                store_row<8>(row + plane, du);
-                store_row<8>(row + 2 * plane, h);
+                gated_put(at, da);
+                gated_put(at + plane, du);
+                gated_put(at + 2 * plane, h);
             }
         }
         if constexpr (P == 1)
@@ -665,81 +710,28 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
         const unsigned char *const sb = lds + Sh::ASLOTS * Sh::A;
         auto slot = [&](int j) { return Sh::ASLOTS == 2 ? ((j - j0) & 1) * Sh::A : 0; };
         auto issue = [&](int j) { gated_stage<Sh::A, WAVES>(ops + (size_t)j * O::CHUNK + O::BIAS, la + slot(j), wave, lane); };
-        if constexpr (Sh::OCC > 1) {
-            GatedHidden<MT> c;
-            issue(j0);
-            start();
+        GatedHidden<MT> c;
+        issue(j0);
+        start();
 #pragma unroll 1
-            for (int j = j0; j < j1; ++j) {
-                wait_vmcnt<0>();
-                barrier();  // (G, U, H)(j) is in LDS; chunk j - 1 is read by all
-                gated_stage<Sh::B, WAVES>(ops + (size_t)j * O::CHUNK + O::XG, lb, wave, lane);
-                const bool more = j + 1 < j1;
-                if (Sh::ASLOTS == 2 && more) issue(j + 1);
-                const unsigned char *const sec = lds + slot(j) + 1024;
-                biases(c, sec - 1024);
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) hidden(c, sec, ks);
-                slopes(c, j, 0, NV);
-                asm volatile("" ::: "memory");
-                if (Sh::ASLOTS == 2 && more) wait_vmcnt<AP + STORES>();
-                else wait_vmcnt<STORES>();
-                barrier();  // (XG, XU)(j) is in LDS, (G, U, H)(j) read by all
-                if (Sh::ASLOTS == 1 && more) issue(j + 1);
-                gated_channels<P, CP, MT, 1>(sb, daf, lane, acc);
-                gated_channels<P, CP, MT, 1>(sb + O::SEC, duf, lane, acc);
-            }
-        } else {
-        // One chunk; `next`, if there is one, gets the following chunk's hidden layer.
-        auto step = [&](GatedHidden<MT> &c, GatedHidden<MT> *next, int j) {
+        for (int j = j0; j < j1; ++j) {
             wait_vmcnt<0>();
-            barrier();  // (G, U, H)(j+1) is in LDS; (G, U, H)(j) and (XG, XU)(j-1) are read by all
+            barrier();  // (G, U, H)(j) is in LDS; chunk j - 1 is read by all
             gated_stage<Sh::B, WAVES>(ops + (size_t)j * O::CHUNK + O::XG, lb, wave, lane);
-            const bool more = j + 2 < j1;
-            if (Sh::ASLOTS == 2 && more) issue(j + 2);
-            if (next) {
-                const unsigned char *const sec = lds + slot(j + 1) + 1024;
-                biases(*next, sec - 1024);
+            const bool more = j + 1 < j1;
+            if (Sh::ASLOTS == 2 && more) issue(j + 1);
+            const unsigned char *const sec = lds + slot(j) + 1024;
+            biases(c, sec - 1024);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    hidden(*next, sec, ks);
-                    slopes(c, j, ks * NV / KS, (ks + 1) * NV / KS);
-                }
-            } else {
-                slopes(c, j, 0, NV);
-            }
+            for (int ks = 0; ks < KS; ++ks) hidden(c, sec, ks);
+            slopes(c, j, 0, NV);
             asm volatile("" ::: "memory");
             if (Sh::ASLOTS == 2 && more) wait_vmcnt<AP + STORES>();
             else wait_vmcnt<STORES>();
-            barrier();  // (XG, XU)(j) is in LDS, (G, U, H)(j+1) read by all
-            if (Sh::ASLOTS == 1 && more) issue(j + 2);
+            barrier();  // (XG, XU)(j) is in LDS, (G, U, H)(j) read by all
+            if (Sh::ASLOTS == 1 && more) issue(j + 1);
             gated_channels<P, CP, MT, 1>(sb, daf, lane, acc);
             gated_channels<P, CP, MT, 1>(sb + O::SEC, duf, lane, acc);
-        };
-        GatedHidden<MT> c0, c1;
-        issue(j0);
-        start();
-        gated_sync();
-        if (Sh::ASLOTS == 2 && j0 + 1 < j1) issue(j0 + 1);
-        biases(c0, lds);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) hidden(c0, lds + 1024, ks);
-        if (Sh::ASLOTS == 1) {
-            barrier();  // (G, U, H)(j0) read by all
-            if (j0 + 1 < j1) issue(j0 + 1);
-        }
-        int j = j0;
-#pragma unroll 1
-        for (; j + 2 < j1; j += 2) {
-            step(c0, &c1, j);
-            step(c1, &c0, j + 1);
-        }
-        if (j + 1 < j1) {
-            step(c0, &c1, j);
-            step(c1, nullptr, j + 1);
-        } else {
-            step(c0, nullptr, j);
-        }
         }
     } else {
         // Step i = 5 (j - j0) + q reads section q of chunk j (bias and G, U, H, XG, XU) from slot
@@ -808,23 +800,26 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
     }
 }
 
-// The backward of wide bfloat16 points in two kernels: their rows (x and g) and the sums of dx
-// fill a wave's registers together, so one wave per SIMD would have to do all (8,900 cycles per
-// chunk at CP = 256, of 2,560 of products); apart, two waves fit, and one's slopes run beside
-// the other's products.  dx then reads da and du back from the store.
-template <int CP> struct GatedWide {
+// Where the rows (x and g) and the sums of dx fill a wave's registers together, one wave per SIMD
+// would have to do all (bfloat16 at CP = 256: 8,900 cycles per chunk, of 2,560 of products;
+// float32 at CP = 128: 350,000 points of F = 512 in 1.53 ms, of 0.68 of products).  There the
+// backward takes two kernels: the slopes without the sums, and dx, which reads da and du back
+// from the store, on two waves per SIMD.
+template <int P, int CP> struct GatedWide {
+    static constexpr bool USE = P == 1 ? CP > 128 : CP == 128;
     static constexpr int WAVES = 4, PTS = WAVES * 32;
-    static constexpr int A = 1024 + 3 * CP * 64, B = 2 * CP * 64;
+    static constexpr int SEC = CP * 64 * P, A = 1024 + 3 * SEC;
 };
 
-// da, du, h and cols of chunks per*s .. of PTS points, as k_gated_dx leaves them.  One LDS
-// slot: the next chunk is copied while the slopes of this one are computed.
+// da, du, h (and cols) of chunks per*s .. of PTS points, as k_gated_dx leaves them, bfloat16.
+// One LDS slot: the next chunk is copied while the slopes of this one are computed, beside the
+// SIMD's other wave.
 template <int CP, int ACT>
 __global__ __launch_bounds__(256, 2) void k_gated_slopes(const bf16_t *__restrict__ x, const bf16_t *__restrict__ g,
                                                          int64_t n, int C, const unsigned char *__restrict__ ops,
                                                          int nchunk, int per, int S, int64_t tp,
                                                          bf16_t *__restrict__ store, float *__restrict__ cols) {
-    using Sh = GatedWide<CP>;
+    using Sh = GatedWide<1, CP>;
     using O = GatedOps<1, CP, 32>;
     constexpr int WAVES = Sh::WAVES, KS = O::KS;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[Sh::A];
@@ -849,7 +844,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_slopes(const bf16_t *__restric
     Rows32<32> a[1], u[1], dh[1];
     auto slopes = [&](int j) {
         asm volatile("" ::: "memory");
-        bf16_t *const row = store + ((int64_t)j * tp + p) * 32 + 16 * (lane / 32);
+        bf16_t *const at = store + ((int64_t)j * tp + p0) * 32 + lane * 8;
         GatedColumns sums;
 #pragma unroll
         for (int v0 = 0; v0 < 16; v0 += 8) {
@@ -864,9 +859,9 @@ __global__ __launch_bounds__(256, 2) void k_gated_slopes(const bf16_t *__restric
                 da[v] = d * uv * slope;
                 sums.add(v0 + v, da[v], du[v]);
             }
-            store_row<8>(row + v0, da);
-            store_row<8>(row + plane + v0, du);
-            store_row<8>(row + 2 * plane + v0, h);
+            gated_put(at + v0 * 64, da);
+            gated_put(at + plane + v0 * 64, du);
+            gated_put(at + 2 * plane + v0 * 64, h);
         }
         sums.store(cols, nchunk, j, tp / 32, p0 / 32, lane);
         asm volatile("" ::: "memory");
@@ -894,66 +889,229 @@ __global__ __launch_bounds__(256, 2) void k_gated_slopes(const bf16_t *__restric
     }
 }
 
-// dx = da Wg^T + du Wu^T from the store, over chunks per*s ..; sums to dx or part as k_gated_fwd.
-// A chunk's da and du of a point lie in the store as the lane's operands; they are on their way
-// two chunks ahead, (XG, XU) one.
-template <int CP>
-__global__ __launch_bounds__(256, 2) void k_gated_dx_wide(int64_t n, int C, const unsigned char *__restrict__ ops,
+// The same in float32, on one wave per SIMD, which issues its vector work beside its own products
+// or not at all: the products into the hidden layer of chunk j + 1 are interleaved with the slopes
+// of chunk j, some values after each K step.  Two LDS slots, copies a chunk ahead.
+template <int CP, int ACT>
+__global__ __launch_bounds__(256, 1) void k_gated_slopes3(const float *__restrict__ x, const float *__restrict__ g,
+                                                          int64_t n, int C, const unsigned char *__restrict__ ops,
                                                           int nchunk, int per, int S, int64_t tp,
-                                                          const bf16_t *__restrict__ store, bf16_t *__restrict__ dx,
-                                                          float *__restrict__ part) {
-    using Sh = GatedWide<CP>;
-    using O = GatedOps<1, CP, 32>;
-    constexpr int WAVES = Sh::WAVES, SLOTS = 2, PER = Sh::B / 1024 / WAVES;
-    static_assert(Sh::B % (1024 * WAVES) == 0, "every wave issues as many copies");
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[SLOTS * Sh::B];
+                                                          float *__restrict__ store) {
+    using Sh = GatedWide<3, CP>;
+    using O = GatedOps<3, CP, 32>;
+    constexpr int WAVES = Sh::WAVES, KS = O::KS, NV = 16, STORES = 3 * NV * 4 / 16;
+    static_assert(NV == 2 * KS, "two values beside each K step");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * Sh::A];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int64_t blk = blockIdx.x / S;
     const int split = blockIdx.x % S;
     const int j0 = split * per, j1 = j0 + per < nchunk ? j0 + per : nchunk;
     const int64_t p0 = blk * Sh::PTS + wave * 32, p = p0 + lane % 32;
+    const bool in = p < n;
     const uint32_t la = lds_addr(lds);
-    auto issue = [&](int j) {
-        gated_stage<Sh::B, WAVES>(ops + (size_t)j * O::CHUNK + O::XG, la + (j - j0) % SLOTS * Sh::B, wave, lane);
+    auto slot = [&](int j) { return ((j - j0) & 1) * Sh::A; };
+    auto issue = [&](int j) { gated_stage<Sh::A, WAVES>(ops + (size_t)j * O::CHUNK + O::BIAS, la + slot(j), wave, lane); };
+    issue(j0);
+    Parts<3> xf[1][KS], gf[1][KS];
+    gated_rows<3, CP, 32, 1>(x, p0, n, C, lane, xf);
+    gated_rows<3, CP, 32, 1>(g, p0, n, C, lane, gf);
+    // As in k_gated_dx: odd points' g is negated on the way in and dh back.
+    const uint32_t flip = lane & 1 ? 0x80008000u : 0u;
+    const float sign = lane & 1 ? -1.f : 1.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int s = 0; s < 3; ++s)
+            gf[0][ks].p[s] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, gf[0][ks].p[s]) ^ flip);
+    auto biases = [&](GatedHidden<32> &c, const unsigned char *bias) {
+        gated_bias<32, 1>(bias, 0, lane, c.a);
+        gated_bias<32, 1>(bias, 1, lane, c.u);
+        c.dh[0].zero();
+    };
+    typedef Parts<3> Fragments[3];
+    auto load = [&](Fragments &w, const unsigned char *sec, int ks) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) lds_parts(sec + i * O::SEC, ks, lane, w[i]);
+    };
+    auto hidden = [&](GatedHidden<32> &c, const Fragments &w, int ks, auto beside) {
+        mma_parts_in_turn<32, 3, 3>({&c.a[0].d[0], &c.u[0].d[0], &c.dh[0].d[0]}, w, {&xf[0][ks], &xf[0][ks], &gf[0][ks]},
+                                    beside);
     };
     const int64_t plane = (int64_t)nchunk * tp * 32;
-    auto fetch = [&](int j, Parts<1> (&f)[2][1][2]) {
-        const bf16_t *const row = store + ((int64_t)j * tp + p) * 32 + 16 * (lane / 32);
+    float da[4], du[4], h[4];
+    auto slopes = [&](GatedHidden<32> &c, int j, int v0, int v1) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+        for (int v = v0; v < v1; ++v) {
+            float slope;
+            const float uv = c.u[0].get(v), d = sign * c.dh[0].get(v);
+            const float y = gated_act<3, ACT, true>(c.a[0].get(v), slope);
+            h[v & 3] = in ? y * uv : 0.f;
+            du[v & 3] = d * y;
+            da[v & 3] = d * uv * slope;
+            if ((v & 3) == 3) {
+                float *const at = store + ((int64_t)j * tp + p0) * 32 + (v & ~3) * 64 + lane * 4;
+                store_row<4>(at, da);
+                store_row<4>(at + plane, du);
+                store_row<4>(at + 2 * plane, h);
+            }
+        }
+    };
+    auto barrier = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // Slopes of chunk j in c; `next` gets the hidden layer of chunk j + 1.
+    auto step = [&](GatedHidden<32> &c, GatedHidden<32> &next, int j) {
+        if (j > j0) wait_vmcnt<STORES>();  // the copies of chunk j + 1 are older than the stores of chunk j - 1
+        else wait_vmcnt<0>();
+        barrier();  // chunk j + 1 is in LDS, chunk j read by all
+        if (j + 2 < j1) issue(j + 2);
+        const unsigned char *const sec = lds + slot(j + 1) + 1024;
+        Fragments w[2];
+        load(w[0], sec, 0);
+        biases(next, sec - 1024);
 #pragma unroll
-            for (int s = 0; s < 2; ++s) load_parts(row + m * plane + 8 * s, f[m][0][s]);
+        for (int ks = 0; ks < KS; ++ks) {
+            __builtin_amdgcn_sched_barrier(0);  // K step by K step: left to itself the compiler gathers the slopes
+            if (ks + 1 < KS) load(w[(ks + 1) & 1], sec, ks + 1);
+            hidden(next, w[ks & 1], ks, [&](int q) {
+                const int at = ks * NV / KS + q / 3;
+                if (q % 3 == 1) slopes(c, j, at, at + 1);
+            });
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+    };
+    GatedHidden<32> c0, c1;
+    gated_sync();
+    if (j0 + 1 < j1) issue(j0 + 1);
+    biases(c0, lds);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        Fragments w;
+        load(w, lds + 1024, ks);
+        hidden(c0, w, ks, [](int) {});
+    }
+    int j = j0;
+#pragma unroll 1
+    for (; j + 2 < j1; j += 2) {
+        step(c0, c1, j);
+        step(c1, c0, j + 1);
+    }
+    if (j + 1 < j1) {
+        step(c0, c1, j);
+        slopes(c1, j + 1, 0, NV);
+    } else {
+        slopes(c0, j, 0, NV);
+    }
+}
+
+// Eight values of a point in the store as an operand, as they were loaded.
+template <int P> struct GatedRaw {
+    u32x4 v[P == 1 ? 1 : 2];
+    __device__ __forceinline__ void load(const typename GatedIO<P>::T *p) {
+        v[0] = *reinterpret_cast<const u32x4 *>(p);
+        if constexpr (P == 3) v[1] = *reinterpret_cast<const u32x4 *>(p + 256);
+    }
+    // Makes the compiler wait for the load here: it does not know of the copies that are issued
+    // after this and would wait for some of them at the first use.
+    __device__ __forceinline__ void arrived() {
+        asm volatile("" : "+v"(v[0]));
+        if constexpr (P == 3) asm volatile("" : "+v"(v[1]));
+    }
+    __device__ __forceinline__ void parts(Parts<P> &f) const {
+        if constexpr (P == 1) f.p[0] = __builtin_bit_cast(bf16x8, v[0]);
+        else {
+            float t[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = __uint_as_float(v[i / 4][i & 3]);
+            split8(t, f);
+        }
+    }
+};
+
+// dx = da Wg^T + du Wu^T from the store, over chunks per*s ..; sums to dx or part as k_gated_fwd.
+// A step takes SPS of the sections XG and XU of a chunk: in bfloat16 both, in two LDS slots, the
+// copies issued one step ahead; in float32 one, in three slots, two steps ahead.  A chunk's da and
+// du of a point lie in the store as the lane's operands; they are on their way two steps ahead.
+template <int P, int CP>
+__global__ __launch_bounds__(256, 2) void k_gated_dx_wide(int64_t n, int C, const unsigned char *__restrict__ ops,
+                                                          int nchunk, int per, int S, int64_t tp,
+                                                          const typename GatedIO<P>::T *__restrict__ store,
+                                                          typename GatedIO<P>::T *__restrict__ dx,
+                                                          float *__restrict__ part) {
+    using T = typename GatedIO<P>::T;
+    using Sh = GatedWide<P, CP>;
+    using O = GatedOps<P, CP, 32>;
+    constexpr int WAVES = Sh::WAVES, SPS = P == 1 ? 2 : 1, SLOTS = P == 1 ? 2 : 3, BYTES = SPS * Sh::SEC;
+    constexpr int PER = BYTES / 1024 / WAVES, LOADS = SPS * 2 * (P == 1 ? 1 : 2);
+    static_assert(BYTES % (1024 * WAVES) == 0, "every wave issues as many copies");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[SLOTS * BYTES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int64_t blk = blockIdx.x / S;
+    const int split = blockIdx.x % S;
+    const int j0 = split * per, j1 = j0 + per < nchunk ? j0 + per : nchunk;
+    const int steps = (j1 - j0) * 2 / SPS;
+    const int64_t p0 = blk * Sh::PTS + wave * 32, p = p0 + lane % 32;
+    const uint32_t la = lds_addr(lds);
+    auto issue = [&](int i) {
+        const unsigned char *const src = ops + (size_t)(j0 + i * SPS / 2) * O::CHUNK + O::XG + (i * SPS & 1) * Sh::SEC;
+        gated_stage<BYTES, WAVES>(src, la + i % SLOTS * BYTES, wave, lane);
+    };
+    const int64_t plane = (int64_t)nchunk * tp * 32;
+    typedef GatedRaw<P> Raws[SPS][2];
+    auto fetch = [&](int i, Raws &f) {
+        const T *const at = store + ((int64_t)(j0 + i * SPS / 2) * tp + p0) * 32 + lane * (P == 1 ? 8 : 4);
+#pragma unroll
+        for (int m = 0; m < SPS; ++m)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) f[m][s].load(at + ((i * SPS & 1) + m) * plane + 512 * s);
     };
     Rows32<32> acc[O::CB][1];
 #pragma unroll
     for (int cb = 0; cb < O::CB; ++cb) acc[cb][0].zero();
-    Parts<1> f[3][2][1][2];
-    issue(j0);
-    fetch(j0, f[0]);
-    if (j0 + 1 < j1) fetch(j0 + 1, f[1]);
-    auto step = [&](Parts<1> (&now)[2][1][2], Parts<1> (&then)[2][1][2], int j) {
-        if (j + 1 < j1) wait_vmcnt<4>();  // da and du of chunk j + 1 may be in flight
-        else wait_vmcnt<0>();
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();  // chunk j is in LDS, chunk j - 1 read by all
+    Raws f[3];
+    issue(0);
+    fetch(0, f[0]);
+    if (steps > 1) {
+        if (SLOTS == 3) issue(1);
         asm volatile("" ::: "memory");
-        if (j + 1 < j1) issue(j + 1);
-        if (j + 2 < j1) fetch(j + 2, then);
-        asm volatile("" ::: "memory");
-        const unsigned char *const sec = lds + (j - j0) % SLOTS * Sh::B;
-        gated_channels<1, CP, 32, 1>(sec, now[0], lane, acc);
-        gated_channels<1, CP, 32, 1>(sec + O::SEC, now[1], lane, acc);
-        gated_ahead<0, 4 * O::CB, 6>();
-    };
-    int j = j0;
-#pragma unroll 1
-    for (; j + 2 < j1; j += 3) {
-        step(f[0], f[2], j);
-        step(f[1], f[0], j + 1);
-        step(f[2], f[1], j + 2);
+        fetch(1, f[1]);
     }
-    if (j < j1) step(f[0], f[2], j);
-    if (j + 1 < j1) step(f[1], f[0], j + 1);
+    auto step = [&](Raws &now, Raws &then, int i) {
+        asm volatile("" ::: "memory");
+        // what was issued for step i + 1 may be in flight
+        if (i + 1 < steps) wait_vmcnt<LOADS + (SLOTS == 3 ? PER : 0)>();
+        else wait_vmcnt<0>();
+#pragma unroll
+        for (int m = 0; m < SPS; ++m)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) now[m][s].arrived();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();  // step i's sections are in LDS, step i - 1's read by all
+        asm volatile("" ::: "memory");
+        if (i + SLOTS - 1 < steps) issue(i + SLOTS - 1);
+        if (i + 2 < steps) fetch(i + 2, then);
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int m = 0; m < SPS; ++m) {
+            Parts<P> hf[1][2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) now[m][s].parts(hf[0][s]);
+            gated_channels<P, CP, 32, 1>(lds + i % SLOTS * BYTES + m * Sh::SEC, hf, lane, acc);
+        }
+        if constexpr (P == 1) gated_ahead<0, 4 * O::CB, 6>();
+    };
+    int i = 0;
+#pragma unroll 1
+    for (; i + 2 < steps; i += 3) {
+        step(f[0], f[2], i);
+        step(f[1], f[0], i + 1);
+        step(f[2], f[1], i + 2);
+    }
+    if (i < steps) step(f[0], f[2], i);
+    if (i + 1 < steps) step(f[1], f[0], i + 1);
     if (S > 1) {
         gated_put_sums<CP, 32, 1>(acc, part + (split * (int64_t)(gridDim.x / S) + blk) * Sh::PTS * CP, wave, lane, n - p0);
         return;
@@ -965,7 +1123,7 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx_wide(int64_t n, int C, cons
         if (c >= C) continue;
         float v[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = acc[cb][0].get(i);
+        for (int t = 0; t < 16; ++t) v[t] = acc[cb][0].get(t);
         store_row<16>(dx + p * C + c, v);
     }
 }
@@ -984,12 +1142,14 @@ template <int P, int CP> struct GatedDw {
     static_assert(CP % 64 == 0, "two channel waves share CP evenly");
 };
 
-// One operand whose K slots are points: columns 32 of plane at `plane` (rows of 64 bytes),
-// K slots 8q .. of the 16 points from row r0.  Lanes 0..31 and 32..63 read 256 consecutive
-// bytes each.
-__device__ __forceinline__ bf16x8 plane_tr(const unsigned char *plane, int r0, int lane) {
-    const int j = lane & 15;
-    const unsigned char *lo = plane + (r0 + 8 * (lane >> 5) + (j >> 2)) * 64 + 32 * ((lane >> 4) & 1) + 8 * (j & 3);
+// One operand whose K slots are points: columns 32 of plane at `plane`, K slots 8q .. of the 16
+// points from row r0.  Lanes 0..31 and 32..63 read 256 consecutive bytes each: four rows of 64
+// bytes, or (PIECES) the four 16-byte pieces of the rows one after another, four rows each, in the
+// order columns 0, 16, 8, 24, as they come from the store.
+template <bool PIECES> __device__ __forceinline__ bf16x8 plane_tr(const unsigned char *plane, int r0, int lane) {
+    const int j = lane & 15, h = (lane >> 4) & 1;
+    const unsigned char *lo = plane + (r0 + 8 * (lane >> 5)) * 64 +
+                              (PIECES ? (j & 2) * 64 + h * 64 + (j >> 2) * 16 + 8 * (j & 1) : (j >> 2) * 64 + 32 * h + 8 * (j & 3));
     const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)lo);
     const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(lo + 256));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -1005,7 +1165,7 @@ __device__ __forceinline__ float sum_slots(const bf16x8 &v, float s) {
 }
 // The weight gradients of the tile's points: for m = 0 (dWg), 1 (dWu): sum of da or du times
 // x; for 2 (dWd): of h times g.  Workgroup (m, hidden block hb, split sp) with sp outermost
-// sums points per*sp .. + per - 1 (per a multiple of KP) into part[sp][m][nchunk * 32][CP] and
+// sums points per*sp .. + per - 1 (per a multiple of 32) into part[sp][m][nchunk * 32][CP] and
 // bpart[sp][m][max(nchunk * 32, CP)] (sums of da, du; for m = 2 of g), added to what is there
 // unless `first` (at the end: short chains of sums round less).  Rows past n are read from
 // `zeros` (16 bytes).
@@ -1039,11 +1199,14 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
     const int FP = nchunk * 32, BW = FP > CP ? FP : CP;
 
     // Piece k of a step: 16 points by one plane of 32 columns (P = 1: half k / PL of the points) or
-    // 16 points by 16 columns (P = 3: half k / PL of the plane); lane l takes 16 bytes of row l / 4.
-    // The wave's pieces are a uniform base, which moves on with the steps, and a lane's offset.
+    // 16 points by 16 columns (P = 3: half k / PL of the plane).  Lane l takes 16 bytes of row l / 4
+    // of x and g; of the store, where four lanes in a row are four points, of row hrow.
+    // The wave's pieces are a uniform base, which moves on with the steps (in the store by a block
+    // of 32 points, for P = 3 in two unequal steps), and a lane's offset.
+    const int hrow = (lane >> 4) * 4 + (lane & 3), hq = (lane >> 2) & 3;
     const unsigned char *base[S::PER];
     uint32_t voff[S::PER];
-    int64_t inc[S::PER];
+    int64_t inc[S::PER], inc2[S::PER];
     constexpr int E = (int)sizeof(T);
 #pragma unroll
     for (int i = 0; i < S::PER; ++i) {
@@ -1054,13 +1217,14 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
             int ch = hb * HPL + pl;
             ch = ch < nchunk ? ch : nchunk - 1;  // its products are not stored
             base[i] = (const unsigned char *)(hid + ((int64_t)ch * tp + a0) * 32);
-            voff[i] = (row * 32 + col) * E;
-            inc[i] = KP * 32 * E;
+            voff[i] = (P == 1 ? gated_at<P>(16 * half + hrow, 16 * (hq & 1) + 8 * (hq >> 1)) : gated_at<P>(hrow, 16 * half + 4 * hq)) * E;
+            inc[i] = P == 1 ? 1024 * E : gated_at<P>(16, 0) * E;
+            inc2[i] = 1024 * E - inc[i];
         } else {  // channels past C repeat others; their products are not stored
             const int c = 32 * (pl - HPL) < C ? 32 * (pl - HPL) : 0;
             base[i] = (const unsigned char *)(cols + a0 * C + c);
             voff[i] = (row * C + (c + col < C ? col : col & 15)) * E;
-            inc[i] = (int64_t)KP * C * E;
+            inc[i] = inc2[i] = (int64_t)KP * C * E;
         }
     }
     // Address of piece i at step k for a step that passes row n, by lane.
@@ -1096,7 +1260,7 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
-                    af[t].p[p] = plane_tr(slot + ((2 * hi + t) * P + p) * S::PLB, r0, lane);
+                    af[t].p[p] = plane_tr<P == 1>(slot + ((2 * hi + t) * P + p) * S::PLB, r0, lane);
                     if constexpr (P == 3 && SUMS == 1) bs[t] = sum_slots(af[t].p[p], bs[t]);
                 }
 #pragma unroll
@@ -1104,7 +1268,7 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
                 Parts<P> bf;
 #pragma unroll
                 for (int p = 0; p < P; ++p) {
-                    bf.p[p] = plane_tr(slot + ((HPL + ci * CTW + c) * P + p) * S::PLB, r0, lane);
+                    bf.p[p] = plane_tr<false>(slot + ((HPL + ci * CTW + c) * P + p) * S::PLB, r0, lane);
                     if constexpr (SUMS == 2) gs[c] = sum_slots(bf.p[p], gs[c]);
                 }
 #pragma unroll
@@ -1149,14 +1313,15 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
 #pragma unroll
             for (int i = 0; i < S::PER; ++i) {
                 st[i] = *reinterpret_cast<const f32x4 *>(whole ? base[i] + voff[i] : ragged(i, k));
-                base[i] += inc[i];
+                base[i] += k & 1 ? inc2[i] : inc[i];
             }
         };
         auto put = [&](int k) {
 #pragma unroll
             for (int i = 0; i < S::PER; ++i) {
                 const int pc = wave * S::PER + i, pl = pc % PL;
-                unsigned char *to = lds + (k % S::SLOTS) * S::SLOT + pl * P * S::PLB + (lane >> 2) * 64 + 32 * (pc / PL) + 8 * (lane & 3);
+                const int at = pl < HPL ? hrow * 64 + 8 * hq : (lane >> 2) * 64 + 8 * (lane & 3);
+                unsigned char *to = lds + (k % S::SLOTS) * S::SLOT + pl * P * S::PLB + at + 32 * (pc / PL);
                 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
                 u32x2 w[3];
 #pragma unroll

@@ -159,7 +159,7 @@ ts3_status ts3_gated_create(const ts3_gated_desc *desc, ts3_gated **out) {
         constexpr int P = decltype(p)::value, CP = decltype(cp)::value;
         const int64_t ops = (int64_t)h->nchunk * GatedOps<P, CP, GatedShape<P, CP>::MT>::CHUNK;
         // a round of workgroups of the kernel with the largest blocks of points
-        const int64_t part = (int64_t)device_cu_count() * std::max(GatedShape<P, CP>::PTS, GatedWide<CP>::PTS) * CP * 4;
+        const int64_t part = (int64_t)device_cu_count() * std::max(GatedShape<P, CP>::PTS, GatedWide<P, CP>::PTS) * CP * 4;
         ts3_status st = device_alloc((void **)&h->ops, ops);
         if (st == TS3_OK) st = device_alloc((void **)&h->bd, CP * 4);
         if (st == TS3_OK) st = device_alloc((void **)&h->part, part);
@@ -268,8 +268,8 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
         constexpr int P = decltype(p)::value, CP = decltype(cp)::value;
         using T = typename GatedIO<P>::T;
         using Dw = GatedDw<P, CP>;
-        constexpr bool WIDE = P == 1 && CP > 128;
-        constexpr int PTS = WIDE ? GatedWide<CP>::PTS : GatedShapeX<P, CP>::PTS;
+        constexpr bool WIDE = GatedWide<P, CP>::USE;
+        constexpr int PTS = WIDE ? GatedWide<P, CP>::PTS : GatedShapeX<P, CP>::PTS;
         const int C = h->desc.C, F = h->desc.F, nchunk = h->nchunk, FP = nchunk * 32, BW = std::max(FP, CP);
         const int nhb = (FP + Dw::HB - 1) / Dw::HB;
         hipStream_t st = (hipStream_t)stream;
@@ -313,11 +313,18 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
             const bool silu = h->desc.activation == TS3_SILU;
             float *const cols = P == 1 ? (float *)((T *)h->store + tp * 3 * FP) : nullptr;
             if constexpr (WIDE) {
-                const auto slopes = silu ? &k_gated_slopes<CP, GATED_SILU> : &k_gated_slopes<CP, GATED_GELU>;
-                hipLaunchKernelGGL(slopes, dim3((unsigned)(nb * S)), dim3(256), 0, st, xt, gt, m, C, h->ops, nchunk, per,
-                                   S, tp, (T *)h->store, cols);
+                const dim3 grid((unsigned)(nb * S));
+                if constexpr (P == 1) {
+                    const auto slopes = silu ? &k_gated_slopes<CP, GATED_SILU> : &k_gated_slopes<CP, GATED_GELU>;
+                    hipLaunchKernelGGL(slopes, grid, dim3(256), 0, st, xt, gt, m, C, h->ops, nchunk, per, S, tp,
+                                       (T *)h->store, cols);
+                } else {
+                    const auto slopes = silu ? &k_gated_slopes3<CP, GATED_SILU> : &k_gated_slopes3<CP, GATED_GELU>;
+                    hipLaunchKernelGGL(slopes, grid, dim3(256), 0, st, xt, gt, m, C, h->ops, nchunk, per, S, tp,
+                                       (T *)h->store);
+                }
                 LAUNCH_CHECK("gated slopes");
-                hipLaunchKernelGGL(k_gated_dx_wide<CP>, dim3((unsigned)(nb * S)), dim3(256), 0, st, m, C, h->ops, nchunk,
+                hipLaunchKernelGGL((k_gated_dx_wide<P, CP>), grid, dim3(256), 0, st, m, C, h->ops, nchunk,
                                    per, S, tp, (const T *)h->store, dxt, h->part);
             } else {
                 const auto kernel = silu ? &k_gated_dx<P, CP, GATED_SILU> : &k_gated_dx<P, CP, GATED_GELU>;
@@ -330,7 +337,7 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
                                    dim3(256), 0, st, h->part, m, C, S, (int)nb, (const float *)nullptr, dxt);
                 LAUNCH_CHECK("gated join");
             }
-            const int64_t pps = ((tp + SP - 1) / SP + Dw::KP - 1) / Dw::KP * Dw::KP;
+            const int64_t pps = ((tp + SP - 1) / SP + 31) / 32 * 32;
             const GatedDwArgs<P, CP> a{xt, gt, (const T *)h->store, cols, m, tp, pps, C, nchunk, nhb, t0 == 0, zeros, h->wpart,
                                        h->bpart};
             hipLaunchKernelGGL((k_gated_dw<P, CP>), dim3((unsigned)(3 * nhb * SP)), dim3(256), 0, st, a);
