@@ -101,13 +101,7 @@ __device__ __forceinline__ void mma_parts_in_turn(typename Mat<MT>::D *const (&d
 template <int MT, int P, int N>
 __device__ __forceinline__ void mma_parts_in_turn(typename Mat<MT>::D *const (&d)[N], const Parts<P> (&a)[N],
                                                   const Parts<P> *const (&b)[N]) {
-    using PP = PartProducts<P, P>;
-#pragma unroll
-    for (int q = 0; q < PP::N; ++q) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) Mat<MT>::mma(*d[i], a[i].p[PP::I[q]], b[i]->p[PP::J[q]]);
-        if constexpr (P > 1) __builtin_amdgcn_sched_barrier(0x096);
-    }
+    mma_parts_in_turn<MT, P, N>(d, a, b, [](int) {});
 }
 template <int MT, int P>
 __device__ __forceinline__ void mma_parts(typename Mat<MT>::D &d, const Parts<P> &a, const Parts<P> &b) {
@@ -591,8 +585,9 @@ struct GatedColumns {
 
 // The store holds da, du and h (m = 0, 1, 2) by chunks and blocks of 32 points, each as the lanes
 // of a 32 x 32 result hold it, 16 bytes of every lane after another: store[m][chunk][tp / 32][1024],
-// so that a wave writes and reads whole lines.  (By rows of 32 hidden units, 16 bytes of a lane to
-// a row, the requests bound every kernel that touches it: STORE_GAIN.)
+// so that a wave writes and reads whole lines.  By rows of 32 hidden units, 16 bytes of a lane to a
+// row, the slopes of 350,000 float32 points at C = 128, F = 512 took 1.03 ms instead of 0.90, a
+// training step of 100,000 at C = 64 336 us instead of 291.
 // Place in its block of hidden unit h (a multiple of the 16 bytes' values) of point p.
 template <int P> __host__ __device__ constexpr int gated_at(int p, int h) {
     constexpr int V = P == 1 ? 8 : 4;
@@ -610,8 +605,9 @@ template <int MT> struct GatedHidden {
     Rows32<MT> a[1], u[1], dh[1];
 };
 
-// dx of n points (the first nb * PTS of the store's), and da, du, h in the store; values of points past n are zero.  In bfloat16 also
-// the sums of da and du over 32 points each, in cols (GatedColumns).  Grid and splits as k_gated_fwd.
+// dx of n points (the first nb * PTS of the store's), and da, du, h in the store; values of points
+// past n are zero.  In bfloat16 also the sums of da and du over 32 points each, in cols
+// (GatedColumns).  Grid and splits as k_gated_fwd.
 // (G, U, H) have two LDS slots where they fit, else one, (XG, XU) have one; copies are issued a
 // phase ahead.
 template <int P, int CP, int ACT>
@@ -673,7 +669,7 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
         }
     };
     // da, du and h of values v0 .. v1 - 1 of chunk j; each eight, as they are complete, become
-    // the next products' operands and 16 or 32 bytes of the store's rows.
+    // the next products' operands and go to the store.
     float da[8], du[8], h[8];
     GatedColumns sums;
     auto slopes = [&](GatedHidden<MT> &c, int j, int v0, int v1) {
@@ -804,7 +800,7 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
 // would have to do all (bfloat16 at CP = 256: 8,900 cycles per chunk, of 2,560 of products;
 // float32 at CP = 128: 350,000 points of F = 512 in 1.53 ms, of 0.68 of products).  There the
 // backward takes two kernels: the slopes without the sums, and dx, which reads da and du back
-// from the store, on two waves per SIMD.
+// from the store, on two waves per SIMD (float32: 0.88 + 0.47 ms).
 template <int P, int CP> struct GatedWide {
     static constexpr bool USE = P == 1 ? CP > 128 : CP == 128;
     static constexpr int WAVES = 4, PTS = WAVES * 32;
@@ -1129,17 +1125,25 @@ __global__ __launch_bounds__(256, 2) void k_gated_dx_wide(int64_t n, int C, cons
 }
 
 // Shape of the weight gradients' kernel: a wave's result is 64 hidden units by CTW tiles of
-// 32 channels, four waves cover HB hidden units by CP channels.
-template <int P, int CP> struct GatedDw {
-    static constexpr int WC = CP > 128 ? 2 : 1, WH = 4 / WC, HB = 64 * WH, CTW = CP / 32 / WC;
+// 32 channels, W waves cover HB hidden units by CP channels.
+// Four waves leave room for two workgroups per compute unit; eight, one workgroup of as many waves,
+// read two thirds of the bytes per product and have LDS for copies three steps ahead instead of
+// two (USE8: bfloat16, where the copies go to LDS directly, at the widths whose pieces divide by
+// eight): 250,000 points at C = 256, F = 1024 took 517 us instead of 548.
+template <int P, int CP, int W> struct GatedDw {
+    static constexpr int WC = CP > 128 ? 2 : 1, WH = W / WC, HB = 64 * WH, CTW = CP / 32 / WC;
     static constexpr int HPL = HB / 32, PL = HPL + CP / 32;  // planes of 32 columns
     static constexpr int KP = P == 1 ? 32 : 16;              // points per step
-    static constexpr int SLOTS = P == 1 ? 3 : 2;
+    static constexpr int SLOTS = P == 3 ? 2 : W == 8 ? 4 : 3;
     static constexpr int PLB = KP * 64;                      // bytes of a plane (of one part)
     static constexpr int SLOT = PL * PLB * P;
-    static constexpr int PIECES = P == 1 ? PL * 2 : PL * 2;  // 1 KiB copies (P = 1), 16-row-by-64-byte loads
-    static constexpr int PER = (PIECES + 3) / 4;
+    static constexpr int PIECES = PL * 2;                    // 1 KiB copies (P = 1), 16-row-by-64-byte loads
+    static constexpr int PER = PIECES / W;
     static_assert(CP % 64 == 0, "two channel waves share CP evenly");
+    static_assert(PIECES % W == 0, "every wave issues as many copies or loads");
+};
+template <int P, int CP> struct GatedDwWide {
+    static constexpr bool USE8 = P == 1 && CP % 128 == 0;
 };
 
 // One operand whose K slots are points: columns 32 of plane at `plane`, K slots 8q .. of the 16
@@ -1181,10 +1185,10 @@ template <int P, int CP> struct GatedDwArgs {
     const unsigned char *zeros;
     float *part, *bpart;
 };
-template <int P, int CP, int SUMS>
+template <int P, int CP, int W, int SUMS>
 __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned char *lds, int m, int hb, int sp) {
     using T = typename GatedIO<P>::T;
-    using S = GatedDw<P, CP>;
+    using S = GatedDw<P, CP, W>;
     constexpr int KP = S::KP, HPL = S::HPL, PL = S::PL, CTW = S::CTW;
     const int64_t n = A.n, tp = A.tp, per = A.per;
     const int C = A.C, nchunk = A.nchunk, first = A.first;
@@ -1272,7 +1276,7 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
                     if constexpr (SUMS == 2) gs[c] = sum_slots(bf.p[p], gs[c]);
                 }
 #pragma unroll
-                for (int t = 0; t < 2; ++t) mma_parts<32, P>(acc[t][c], af[t], bf);
+                for (int t = 0; t < 2; ++t) mma_parts<32, P>(acc[t][c], af[t], bf);  // in turn they gain nothing here
             }
         }
 #pragma unroll
@@ -1293,17 +1297,18 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
                 base[i] += inc[i];
             }
         };
-        static_assert(S::PIECES % 4 == 0, "every wave issues as many copies");
-        if (nk > 0) issue(0);
-        if (nk > 1) issue(1);
+        constexpr int AHEAD = S::SLOTS - 1;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (k < nk) issue(k);
 #pragma unroll 1
         for (int k = 0; k < nk; ++k) {
-            if (k + 1 < nk) wait_vmcnt<S::PER>();
+            if (k + AHEAD - 1 < nk) wait_vmcnt<(AHEAD - 1) * S::PER>();
             else wait_vmcnt<0>();
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();  // step k is in LDS; step k - 1's slot read by all
             asm volatile("" ::: "memory");
-            if (k + 2 < nk) issue(k + 2);
+            if (k + AHEAD < nk) issue(k + AHEAD);
             step(k);
         }
     } else {
@@ -1338,7 +1343,6 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
                 for (int p = 0; p < P; ++p) *reinterpret_cast<u32x2 *>(to + p * S::PLB) = w[p];
             }
         };
-        static_assert(S::PIECES % 4 == 0, "every wave loads as many pieces");
         if (nk > 0) {
             fetch(0);
             put(0);
@@ -1374,7 +1378,7 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
     if constexpr (P == 1 && SUMS == 1) {
         // Rows of 32 points and chunks of the split: eight lanes a row, TPC a chunk.
         static_assert(KP == 32, "a split is whole rows of cols");
-        constexpr int TPC = 256 / HPL;
+        constexpr int TPC = 64 * W / HPL;
         const int ch = hb * HPL + threadIdx.x / TPC, row = threadIdx.x % TPC / 8, c4 = 4 * (threadIdx.x & 7);
         if (ch < nchunk) {
             const float *const src = A.cols + (((int64_t)m * nchunk + ch) * (tp / 32) + a0 / 32) * 32 + c4;
@@ -1405,14 +1409,15 @@ __device__ __forceinline__ void gated_dw(const GatedDwArgs<P, CP> &A, unsigned c
         }
 }
 
-template <int P, int CP> __global__ __launch_bounds__(256, 2) void k_gated_dw(const GatedDwArgs<P, CP> A) {
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[GatedDw<P, CP>::SLOTS * GatedDw<P, CP>::SLOT];
+template <int P, int CP, int W> __global__ __launch_bounds__(64 * W, 2) void k_gated_dw(const GatedDwArgs<P, CP> A) {
+    using S = GatedDw<P, CP, W>;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[S::SLOTS * S::SLOT];
     // The workgroups of one split, which read the same rows of x and g, share an XCD and its L2.
     const int wid = xcd_remap(blockIdx.x, gridDim.x);
     const int hb = wid % A.nhb, m = wid / A.nhb % 3, sp = wid / (3 * A.nhb);
-    if (m < 2) gated_dw<P, CP, 1>(A, lds, m, hb, sp);
-    else if (hb == 0) gated_dw<P, CP, 2>(A, lds, m, hb, sp);
-    else gated_dw<P, CP, 0>(A, lds, m, hb, sp);
+    if (m < 2) gated_dw<P, CP, W, 1>(A, lds, m, hb, sp);
+    else if (hb == 0) gated_dw<P, CP, W, 2>(A, lds, m, hb, sp);
+    else gated_dw<P, CP, W, 0>(A, lds, m, hb, sp);
 }
 
 // The gradients from the splits' sums: block (hidden tile of 32, channel tile of 32, m), four

@@ -53,14 +53,26 @@ int gated_splits(int64_t n, int64_t nb, int nchunk, int P, int CP) {
     return (nchunk + per - 1) / per;
 }
 
-// Splits of the points for the weight gradients: at most two workgroups per compute unit in
-// all.  A split costs its sums, 3 F C floats written and read at 2.5 TB/s together, and saves
+// Waves of the weight gradients' workgroups: eight where they cover the hidden units with no more
+// than an eighth of their products on units that do not exist.
+template <int P, int CP> int gated_dw_waves(int nchunk) {
+    if constexpr (GatedDwWide<P, CP>::USE8) {
+        constexpr int HB = GatedDw<P, CP, 8>::HB;
+        const int F = nchunk * 32, covered = (F + HB - 1) / HB * HB;
+        if (8 * (covered - F) <= covered) return 8;
+    }
+    return 4;
+}
+
+// Splits of the points for the weight gradients: at most eight waves per compute unit in all.  A
+// split costs its sums, 3 F C floats written and read at 2.5 TB/s together, and saves
 // steps of KP points (0.6 us each, 0.8 in float32), so few points take fewer: of 3,000 at C =
 // 256, F = 1024 in bfloat16, 21 splits took 34 us with their sums, 7 take 22.
 template <int P, int CP> int gated_point_splits(int nchunk, int64_t points) {
-    using Dw = GatedDw<P, CP>;
-    const int nhb = (nchunk * 32 + Dw::HB - 1) / Dw::HB;
-    const int64_t most = std::max<int64_t>(1, (int64_t)2 * device_cu_count() / (3 * nhb));
+    using Dw = GatedDw<P, CP, 4>;
+    const int W = gated_dw_waves<P, CP>(nchunk), HB = Dw::HB / 4 * W;
+    const int nhb = (nchunk * 32 + HB - 1) / HB;
+    const int64_t most = std::max<int64_t>(1, (int64_t)(8 / W) * device_cu_count() / (3 * nhb));
     const double steps = (double)points / Dw::KP * (P == 1 ? 0.6 : 0.8), sums = 3.0 * nchunk * 32 * CP * 4 / 2.5e6;
     return (int)std::min<int64_t>(most, std::max<int64_t>(1, (int64_t)std::ceil(std::sqrt(steps / sums))));
 }
@@ -267,11 +279,10 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
     return gated_dispatch(h, [&](auto p, auto cp) -> ts3_status {
         constexpr int P = decltype(p)::value, CP = decltype(cp)::value;
         using T = typename GatedIO<P>::T;
-        using Dw = GatedDw<P, CP>;
         constexpr bool WIDE = GatedWide<P, CP>::USE;
         constexpr int PTS = WIDE ? GatedWide<P, CP>::PTS : GatedShapeX<P, CP>::PTS;
         const int C = h->desc.C, F = h->desc.F, nchunk = h->nchunk, FP = nchunk * 32, BW = std::max(FP, CP);
-        const int nhb = (FP + Dw::HB - 1) / Dw::HB;
+        const int W = gated_dw_waves<P, CP>(nchunk), HB = GatedDw<P, CP, 4>::HB / 4 * W, nhb = (FP + HB - 1) / HB;
         hipStream_t st = (hipStream_t)stream;
         // k_gated_load leaves zeros after the 64 biases of a chunk's block.
         const unsigned char *const zeros = h->ops + GatedOps<P, CP, GatedShape<P, CP>::MT>::BIAS + 256;
@@ -340,7 +351,10 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
             const int64_t pps = ((tp + SP - 1) / SP + 31) / 32 * 32;
             const GatedDwArgs<P, CP> a{xt, gt, (const T *)h->store, cols, m, tp, pps, C, nchunk, nhb, t0 == 0, zeros, h->wpart,
                                        h->bpart};
-            hipLaunchKernelGGL((k_gated_dw<P, CP>), dim3((unsigned)(3 * nhb * SP)), dim3(256), 0, st, a);
+            auto dw = &k_gated_dw<P, CP, 4>;
+            if constexpr (GatedDwWide<P, CP>::USE8)
+                if (W == 8) dw = &k_gated_dw<P, CP, 8>;
+            hipLaunchKernelGGL(dw, dim3((unsigned)(3 * nhb * SP)), dim3(64 * W), 0, st, a);
             LAUNCH_CHECK("gated weight gradients");
         }
         hipLaunchKernelGGL((k_gated_grads<P, CP>), dim3(nchunk, (C + 31) / 32, 3), dim3(1024), 0, st, h->wpart, h->bpart,
