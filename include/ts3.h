@@ -358,7 +358,9 @@ ts3_status ts3_stack_feedforward(ts3_stack *s, const ts3_block_weights *blocks, 
  *     a = x Wg + bg,  u = x Wu + bu,  out = (act(a) * u) Wd + bd
  *  C         : a multiple of 16, at most 256; F from 1 to 65536 (any value).
  *              Beyond: TS3_ERR_UNSUPPORTED.
- *  activation: SiLU a / (1 + e^-a), or GELU a Phi(a).
+ *  activation: SiLU a / (1 + e^-a), or GELU a Phi(a) (TS3_BF16: Phi from a fit that is
+ *              within 1.3e-4 of each value down to a = -13, a fifteenth of a bfloat16
+ *              rounding; the same in the forward and the backward).
  *  io_dtype  : ts3_dtype of everything the operator takes and gives: x, out,
  *              g, dx, weights, biases and their gradients.  TS3_BF16 computes
  *              on bf16 matrix cores with float32 sums and rounds each hidden

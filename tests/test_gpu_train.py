@@ -172,6 +172,30 @@ def test_gated_gates_that_are_nearly_closed(gate, kind, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+@pytest.mark.parametrize("gate", [-5.5, -6.0, -7.0, -8.0, -10.0])
+def test_gated_gates_far_down_the_tail(gate, kind, dtype):
+    """As above, further down, and every gradient.  A relative change of a by d changes GELU and its
+    slope by about a^2 d of themselves, so float32's walk of the sums over C counts a^2 times; in
+    bfloat16 that is still far below a rounding."""
+    import torch
+    from oracle import train as T
+    N, C, F = 200, 96, 70
+    x, w, g = _gated(N, C, F, dtype, True, seed=7, scale=0.05)
+    w["bg"], w["bd"] = np.full(F, gate), np.zeros(C)
+    with _operator(C, F, kind, dtype, w) as ff:
+        xt = to_device(x, dtype)
+        out = ff.forward(xt)
+        dx, grads = ff.backward(xt, to_device(g, dtype))
+        torch.cuda.synchronize()
+    _check("out", out, T.gated_forward(x, w, kind), dtype, (C * gate ** 4, F))
+    ref = T.gated_backward(x, w, kind, g)
+    _check("dx", dx, ref["dx"], dtype, (C * gate ** 4, F))
+    for n in NAMES:
+        _check(n, grads[n], ref[n], dtype, (C * gate ** 4, F, N))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("N", [5, 300, 50_000])
 def test_gated_rows_are_independent(N, dtype):
     """A row of NaN and one of infinities stay where they are, also at the end of the call."""
