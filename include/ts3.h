@@ -352,7 +352,11 @@ ts3_status ts3_stack_feedforward(ts3_stack *s, const ts3_block_weights *blocks, 
  * calls on one handle share them, so they belong on one stream (or on streams
  * ordered by events), and a handle on one device.  A handle serves calls of
  * any n.  As for the layer, the calls only enqueue work; create, free and
- * the growth noted at ts3_gated_backward may synchronise. */
+ * the growth noted at ts3_gated_backward may synchronise.  The calls may be
+ * captured into a graph, whose replays need the handle: a buffer that a capture
+ * has used is kept until the handle is freed, also where a later call grows past
+ * it.  A call that would have to allocate inside a capture does nothing and
+ * gives BAD_STATE: run it once before. */
 
 /* Gated feed-forward over points x [n, C] with hidden width F:
  *     a = x Wg + bg,  u = x Wu + bu,  out = (act(a) * u) Wd + bd
@@ -418,7 +422,9 @@ ts3_status ts3_gated_forward(ts3_gated *h, const void *x, int64_t n, void *out, 
  * 3 F min(tile, n) elements (in bfloat16 1/24 more, for sums of da and du as they
  * are before their rounding) between the kernels that make and use them.
  * The store is allocated by the first call, or a later one that needs more
- * (this synchronises; TS3_ERR_OUT_OF_MEMORY if it does not fit), and kept.
+ * (this synchronises; TS3_ERR_OUT_OF_MEMORY if it does not fit), and kept.  So
+ * are the sums of the weight gradients' splits, by the first call alone: 3 F C
+ * floats (F and C padded to 32 and 64) for each split, some tens of MB.
  * Sums over points are in a fixed order for given n and tile.  n == 0 writes
  * zero gradients. */
 ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_t n, int64_t tile, void *dx,

@@ -397,6 +397,8 @@ int64_t zp_bytes(const ts3_desc &d, bool rt) {
 
 }  // namespace
 
+#include "ts3_workspace.h"
+
 struct ts3_state {
     ts3_desc desc;
     Kernels k;

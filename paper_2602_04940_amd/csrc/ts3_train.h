@@ -13,10 +13,10 @@ struct ts3_gated {
     unsigned char *ops = nullptr;  // GatedOps
     float *bd = nullptr;           // [CP]
     float *part = nullptr;         // sums of split outputs, a sheet of PTS x CP per workgroup
-    void *store = nullptr;         // da, du, h of a tile
-    float *wpart = nullptr;        // sums of the weight gradients' splits
-    float *bpart = nullptr;        // and of the biases'
-    int64_t store_bytes = 0, bytes = 0;
+    Workspace store;               // da, du, h of a tile
+    Workspace wpart;               // sums of the weight gradients' splits
+    Workspace bpart;               // and of the biases'
+    int64_t bytes = 0;
 };
 struct ts3_norm {
     ts3_norm_desc desc{};
@@ -79,14 +79,6 @@ template <int P, int CP> int gated_point_splits(int nchunk, int64_t points) {
 
 constexpr int64_t GATED_TILE_MAX = 1 << 24;
 
-ts3_status device_alloc(void **p, int64_t bytes) {
-    hipError_t e = hipMalloc(p, (size_t)bytes);
-    if (e == hipSuccess) return TS3_OK;
-    (void)hipGetLastError();
-    *p = nullptr;
-    return fail(e == hipErrorOutOfMemory ? TS3_ERR_OUT_OF_MEMORY : TS3_ERR_HIP, "hipMalloc(%lld bytes): %s",
-                (long long)bytes, hipGetErrorString(e));
-}
 bool aligned16(std::initializer_list<const void *> ps) {
     for (const void *p : ps)
         if ((uintptr_t)p & 15) return false;
@@ -189,8 +181,8 @@ ts3_status ts3_gated_create(const ts3_gated_desc *desc, ts3_gated **out) {
 ts3_status ts3_gated_free(ts3_gated *h) {
     if (!h) return TS3_OK;
     hipError_t e = hipDeviceSynchronize();
-    for (void *p : {(void *)h->ops, (void *)h->bd, (void *)h->part, h->store, (void *)h->wpart, (void *)h->bpart})
-        if (p) (void)hipFree(p);
+    for (void *p : {(void *)h->ops, (void *)h->bd, (void *)h->part}) (void)hipFree(p);
+    for (Workspace *w : {&h->store, &h->wpart, &h->bpart}) w->free();
     delete h;
     if (e != hipSuccess) return fail(TS3_ERR_HIP, "hipDeviceSynchronize: %s", hipGetErrorString(e));
     return TS3_OK;
@@ -294,53 +286,38 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
             const int64_t need = rows * 3 * FP * (int64_t)sizeof(T) + (P == 1 ? rows / 32 * 2 * FP * 4 : 0);
             const int most = gated_point_splits<P, CP>(nchunk, GATED_TILE_MAX);
             const int64_t wbytes = (int64_t)most * 3 * FP * CP * 4, bbytes = (int64_t)most * 3 * BW * 4;
-            if (!h->wpart) {
-                ts3_status s = device_alloc((void **)&h->wpart, wbytes);
-                if (s != TS3_OK) return s;
-                h->bytes += wbytes;
-            }
-            if (!h->bpart) {
-                ts3_status s = device_alloc((void **)&h->bpart, bbytes);
-                if (s != TS3_OK) return s;
-                h->bytes += bbytes;
-            }
-            if (h->store_bytes < need) {
-                HIP_TRY(hipDeviceSynchronize());
-                if (h->store) (void)hipFree(h->store);
-                h->store = nullptr;
-                h->bytes -= h->store_bytes;
-                h->store_bytes = 0;
-                ts3_status s = device_alloc(&h->store, need);
-                if (s != TS3_OK) return s;
-                h->store_bytes = need;
-                h->bytes += need;
-            }
+            ts3_status s = h->wpart.reserve(wbytes, st, h->bytes);
+            if (s == TS3_OK) s = h->bpart.reserve(bbytes, st, h->bytes);
+            if (s == TS3_OK) s = h->store.reserve(need, st, h->bytes);
+            if (s != TS3_OK) return s;
         }
+        T *const store = (T *)h->store.p;
+        float *const wpart = (float *)h->wpart.p, *const bpart = (float *)h->bpart.p;
         for (int64_t t0 = 0; t0 < n; t0 += step) {
             const int64_t m = std::min(step, n - t0), nb = (m + PTS - 1) / PTS, tp = nb * PTS;
             const int S = gated_splits(m, nb, nchunk, P, CP), per = (nchunk + S - 1) / S;
             const T *const xt = (const T *)x + t0 * C, *const gt = (const T *)g + t0 * C;
             T *const dxt = (T *)dx + t0 * C;
             const bool silu = h->desc.activation == TS3_SILU;
-            float *const cols = P == 1 ? (float *)((T *)h->store + tp * 3 * FP) : nullptr;
+            float *const cols = P == 1 ? (float *)(store + tp * 3 * FP) : nullptr;
             if constexpr (WIDE) {
                 const dim3 grid((unsigned)(nb * S));
                 if constexpr (P == 1) {
                     const auto slopes = silu ? &k_gated_slopes<CP, GATED_SILU> : &k_gated_slopes<CP, GATED_GELU>;
                     hipLaunchKernelGGL(slopes, grid, dim3(256), 0, st, xt, gt, m, C, h->ops, nchunk, per, S, tp,
-                                       (T *)h->store, cols);
+                                       store, cols);
                 } else {
                     const auto slopes = silu ? &k_gated_slopes3<CP, GATED_SILU> : &k_gated_slopes3<CP, GATED_GELU>;
                     hipLaunchKernelGGL(slopes, grid, dim3(256), 0, st, xt, gt, m, C, h->ops, nchunk, per, S, tp,
-                                       (T *)h->store);
+                                       store);
                 }
                 LAUNCH_CHECK("gated slopes");
                 hipLaunchKernelGGL((k_gated_dx_wide<P, CP>), grid, dim3(256), 0, st, m, C, h->ops, nchunk,
-                                   per, S, tp, (const T *)h->store, dxt, h->part);
+                                   per, S, tp, (const T *)store, dxt, h->part);
             } else {
                 const auto kernel = silu ? &k_gated_dx<P, CP, GATED_SILU> : &k_gated_dx<P, CP, GATED_GELU>;
                 hipLaunchKernelGGL(kernel, dim3((unsigned)(nb * S)), dim3(256), 0, st, xt, gt, m, C, h->ops, nchunk, per,
-                                   S, tp, (T *)h->store, cols, dxt, h->part);
+                                   S, tp, store, cols, dxt, h->part);
             }
             LAUNCH_CHECK("gated dx");
             if (S > 1) {
@@ -349,15 +326,14 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
                 LAUNCH_CHECK("gated join");
             }
             const int64_t pps = ((tp + SP - 1) / SP + 31) / 32 * 32;
-            const GatedDwArgs<P, CP> a{xt, gt, (const T *)h->store, cols, m, tp, pps, C, nchunk, nhb, t0 == 0, zeros, h->wpart,
-                                       h->bpart};
+            const GatedDwArgs<P, CP> a{xt, gt, store, cols, m, tp, pps, C, nchunk, nhb, t0 == 0, zeros, wpart, bpart};
             auto dw = &k_gated_dw<P, CP, 4>;
             if constexpr (GatedDwWide<P, CP>::USE8)
                 if (W == 8) dw = &k_gated_dw<P, CP, 8>;
             hipLaunchKernelGGL(dw, dim3((unsigned)(3 * nhb * SP)), dim3(64 * W), 0, st, a);
             LAUNCH_CHECK("gated weight gradients");
         }
-        hipLaunchKernelGGL((k_gated_grads<P, CP>), dim3(nchunk, (C + 31) / 32, 3), dim3(1024), 0, st, h->wpart, h->bpart,
+        hipLaunchKernelGGL((k_gated_grads<P, CP>), dim3(nchunk, (C + 31) / 32, 3), dim3(1024), 0, st, wpart, bpart,
                            SP, nchunk, C, F, (T *)gr->dWg, (T *)gr->dWu, (T *)gr->dWd, (T *)gr->dbg, (T *)gr->dbu,
                            (T *)gr->dbd);
         LAUNCH_CHECK("gated gradient sums");

@@ -509,3 +509,71 @@ def test_on_another_stream_and_in_a_graph(dtype):
                 torch.cuda.synchronize()
                 for i, (a, b) in enumerate(zip(eager, captured)):
                     assert torch.equal(a, b), (n, seed, i)
+
+
+@pytest.mark.parametrize("dtype,C", [("fp32", 96), ("bf16", 96), ("bf16", 256)])
+def test_graphs_outlive_a_larger_call(dtype, C):
+    """The store that a captured backward uses is kept when a later call grows past it: the first
+    graph's replays, after two larger calls, still give the eager result."""
+    import torch
+    F = 130
+    _, w, _ = _gated(1, C, F, dtype, True)
+    with _operator(C, F, "silu", dtype, w) as ff:
+        def inputs(n):
+            return [torch.zeros((n, C), device="cuda", dtype=ff.torch_dtype) for _ in range(2)]
+
+        def fill(tensors, seed):
+            gen = torch.Generator(device="cuda").manual_seed(seed)
+            for t in tensors:
+                t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+        small, middle, large = inputs(300), inputs(3000), inputs(9000)
+        for t in (small, middle, large):
+            fill(t, 0)
+        ff.backward(*small)
+        first = ff.bytes()
+        ff.backward(*middle)
+        grown = ff.bytes()
+        element = 2 if dtype == "bf16" else 4
+        assert grown - first >= 2000 * 3 * F * element
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            dx, grads = ff.backward(*middle)
+        ff.backward(*large)
+        # the captured store and the larger one beside it
+        assert ff.bytes() - grown >= 9000 * 3 * F * element
+        for seed in (1, 2, 3):
+            fill(middle, seed)
+            fill(large, seed)
+            edx, egrads = ff.backward(*middle)
+            ff.backward(*large)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(dx, edx) and all(torch.equal(grads[n], egrads[n]) for n in NAMES), seed
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_a_capture_that_would_allocate_is_refused(dtype):
+    import torch
+    from paper_2602_04940_amd import _lib as L
+    C, F, N = 64, 70, 500
+    x, w, g = _gated(N, C, F, dtype, True)
+    with _operator(C, F, "gelu", dtype, w) as ff:
+        xt, gt = to_device(x, dtype), to_device(g, dtype)
+        for ready in (0, 100):  # no call before, and one of fewer points
+            if ready:
+                ff.backward(xt[:ready], gt[:ready])
+            held = ff.bytes()
+            out = torch.empty_like(xt)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                with pytest.raises(L.TS3Error) as e:
+                    ff.backward(xt, gt)
+                ff.forward(xt, out=out)  # the capture goes on
+            assert e.value.status == L.TS3_ERR_BAD_STATE and ff.bytes() == held
+            graph.replay()
+            assert torch.equal(out, ff.forward(xt))
+        dx, grads = ff.backward(xt, gt)
+        dx2, grads2 = ff.backward(xt, gt)
+        torch.cuda.synchronize()
+        assert torch.equal(dx, dx2) and all(torch.equal(grads[n], grads2[n]) for n in NAMES)
