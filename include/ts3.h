@@ -254,6 +254,9 @@ ts3_status ts3_layer_forward_noalloc(const ts3_desc *desc, const ts3_weights *w,
  * min(tile, N)*H*M floats (2 GB for 1M-point tiles at H*M = 512); the first
  * call, or a later one with a larger tile, allocates it and the state keeps
  * it (ts3_state_bytes counts it; TS3_ERR_OUT_OF_MEMORY if it does not fit).
+ * A store that a captured graph uses is kept beside a larger one until the state
+ * is freed; a call that would have to allocate inside a capture does nothing and
+ * gives BAD_STATE.
  * Leaves the state ATTENDED. */
 ts3_status ts3_layer_backward(ts3_state *st, const ts3_weights *w, const void *x, const void *g, int64_t N,
                               int64_t tile, void *dx, const ts3_grads *grads, void *stream);

@@ -416,8 +416,7 @@ struct ts3_state {
     void *bop[4] = {nullptr, nullptr, nullptr, nullptr};  // BwOperands: zr, ds, w2t, dst (float32 only)
     // backward: dz [H][points][M] of one tile, allocated by the first backward
     // whose tile needs more than it holds
-    float *bdz = nullptr;
-    int64_t bdz_points = 0;
+    Workspace bdz;
     void *w2p = nullptr, *zp = nullptr;
     // slice-state form of pass 2: s'^T and W3^T fragments, valid after attention
     // (not after a state injected as Z)
@@ -611,9 +610,10 @@ ts3_status ts3_state_free(ts3_state *st) {
     hipError_t e = hipDeviceSynchronize();
     void *bufs[] = {st->partials, st->runs, st->s_raw, st->dsum, st->s,    st->s1,    st->Z,
                     st->b2s,      st->b3,   st->w2p,   st->zp,   st->bdZ,  st->bdsr,  st->bop[0], st->bop[1],
-                    st->bop[2], st->bop[3], st->bdd, st->bdW2T, st->bdz,  st->sfp,  st->w3p,   st->w1p};
+                    st->bop[2], st->bop[3], st->bdd, st->bdW2T, st->sfp,  st->w3p,    st->w1p};
     for (void *b : bufs)
         if (b) (void)hipFree(b);
+    st->bdz.free();
     if (st->ev_fork) (void)hipEventDestroy(st->ev_fork);
     if (st->ev_join) (void)hipEventDestroy(st->ev_join);
     if (st->aux) (void)hipStreamDestroy(st->aux);
@@ -1039,26 +1039,10 @@ ts3_status ts3_layer_backward(ts3_state *st, const ts3_weights *w, const void *x
     const float *xf = (const float *)x, *gf = (const float *)g;
     const void *w2p = st->w2p;
     const int64_t nt_max = std::min(tile, N);
-    if (st->bdz_points < nt_max) {
-        // dz of one tile, [H][points][M]; kept by the state for later calls
-        if (st->bdz) {
-            HIP_TRY(hipStreamSynchronize(hs));
-            (void)hipFree(st->bdz);
-            st->bdz = nullptr;
-            st->bytes -= st->bdz_points * HM * 4;
-            st->bdz_points = 0;
-        }
-        const size_t bytes = (size_t)(nt_max * HM * 4);
-        hipError_t e = hipMalloc((void **)&st->bdz, bytes);
-        if (e != hipSuccess) {
-            (void)hipGetLastError();
-            st->bdz = nullptr;
-            return fail(e == hipErrorOutOfMemory ? TS3_ERR_OUT_OF_MEMORY : TS3_ERR_HIP,
-                        "hipMalloc(%zu bytes) for the backward's dz: %s", bytes, hipGetErrorString(e));
-        }
-        st->bdz_points = nt_max;
-        st->bytes += (int64_t)bytes;
-    }
+    // dz of one tile, [H][points][M]; kept by the state for later calls
+    ts3_status s = st->bdz.reserve(nt_max * HM * 4, hs, st->bytes);
+    if (s != TS3_OK) return s;
+    float *const dz = (float *)st->bdz.p;
     // dZ = sum_i w_i^T g_i (its column C, sum_i w_i, is not needed)
     st->partials_fwd = false;  // the backward passes reuse the span partial buffer
     for (int64_t t0 = 0; t0 < N; t0 += tile) {
@@ -1067,7 +1051,7 @@ ts3_status ts3_layer_backward(ts3_state *st, const ts3_weights *w, const void *x
                       w2p, st->b2s, st->partials, hs);
         LAUNCH_CHECK("backward dZ pass");
     }
-    ts3_status s = fold_partials(st, st->geo.parts(N), d.C, st->bdZ, st->bdd, hs);
+    s = fold_partials(st, st->geo.parts(N), d.C, st->bdZ, st->bdd, hs);
     if (s != TS3_OK) return s;
     // token side: ds_raw, dd and the Linear1 / attention / Linear3 gradients
     size_t lds = bw_token_lds(d.C, d.M, d.dh, false);
@@ -1089,9 +1073,9 @@ ts3_status ts3_layer_backward(ts3_state *st, const ts3_weights *w, const void *x
     for (int64_t t0 = 0; t0 < N; t0 += tile) {
         const int64_t nt = std::min(tile, N - t0);
         st->k.bw_dx(xf + t0 * d.C, gf + t0 * d.C, nt, d.H, w2p, st->b2s, op, st->bdd, inv_tau, (float *)dx + t0 * d.C,
-                    st->bdz, hs);
+                    dz, hs);
         LAUNCH_CHECK("backward dx pass");
-        st->k.bw_dw2(xf + t0 * d.C, st->bdz, nt, t0 / Q * st->geo.S, st->geo, (int32_t)st->geo.parts(nt), d.H,
+        st->k.bw_dw2(xf + t0 * d.C, dz, nt, t0 / Q * st->geo.S, st->geo, (int32_t)st->geo.parts(nt), d.H,
                      st->partials, hs);
         LAUNCH_CHECK("backward dW2 pass");
     }

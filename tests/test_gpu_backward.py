@@ -97,3 +97,35 @@ def test_backward_with_the_float64_fold_matches_oracle_and_is_tiling_independent
     assert normwise(dx_a, ref["dx"]) <= TOL
     for k in NAMES:
         assert normwise(ga[k], ref[k]) <= TOL, k
+
+
+def test_graph_outlives_a_larger_tile():
+    """The dz store that a captured backward uses is kept when a later call's larger tile grows past
+    it: the graph's replays still give the eager result."""
+    torch = _torch()
+    C, H, M, N, Q = 64, 4, 32, 3000, 256
+    rng = np.random.default_rng(17)
+    W = make_weights(C, H, M, C // H, seed=3, bias_seed=4)
+    lw = _weights(W)
+    x, g = (to_device(rng.standard_normal((N, C)), "fp32") for _ in range(2))
+    with _layer(C, H, M, Q, N) as layer:
+        def step(tile):
+            out = layer.forward(lw, x, tile=2048)
+            return [out] + [t for p in (layer.backward(lw, x, g, tile=tile),) for t in [p[0], *p[1].values()]]
+        step(512)
+        held = layer.bytes()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            captured = step(512)
+        step(2048)
+        assert layer.bytes() - held == 2048 * H * M * 4  # beside the captured one
+        for seed in (1, 2, 3):
+            gen = torch.Generator(device="cuda").manual_seed(seed)
+            for t in (x, g):
+                t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+            eager = [t.clone() for t in step(512)]
+            step(2048)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(eager, captured)), seed
