@@ -411,18 +411,18 @@ ts3_status ts3_gated_bytes(const ts3_gated *h, int64_t *bytes);
  * not read again after the enqueued work. */
 ts3_status ts3_gated_load(ts3_gated *h, const ts3_gated_weights *w, void *stream);
 
-/* out = feed-forward of x, both [n, C], 16-byte aligned; out may be x itself.
- * n == 0 is a no-op.  A point's result does not depend on the other points,
- * but its rounding may depend on n: a call of few points splits the hidden
- * units over workgroups and joins their sums in order.  BAD_STATE before the
- * first load. */
+/* out = feed-forward of x, both [n, C], 16-byte aligned; out may be x itself (an
+ * overlap in part is refused).  n == 0 is a no-op.  A point's result does not
+ * depend on the other points, but its rounding may depend on n: a call of few
+ * points splits the hidden units over workgroups and joins their sums in order.
+ * BAD_STATE before the first load. */
 ts3_status ts3_gated_forward(ts3_gated *h, const void *x, int64_t n, void *out, void *stream);
 
 /* Gradients of sum(g * out) for the x and the loaded weights of the forward
  * (which need not have run: the hidden layer is recomputed).  dx [n, C]
- * (neither x nor g) and the weight gradients.  The points pass in tiles of `tile`
- * (at most 2^24 are taken): a tile's da, du and h stay in a store of
- * 3 F min(tile, n) elements (in bfloat16 1/24 more, for sums of da and du as they
+ * overlaps neither x nor g, and the weight gradients neither one another nor dx
+ * (refused).  The points pass in tiles of `tile` (at most 2^24 are taken): a
+ * tile's da, du and h stay in a store of 3 F min(tile, n) elements (in bfloat16 1/24 more, for sums of da and du as they
  * are before their rounding) between the kernels that make and use them.
  * The store is allocated by the first call, or a later one that needs more
  * (this synchronises; TS3_ERR_OUT_OF_MEMORY if it does not fit), and kept.  So
@@ -448,13 +448,14 @@ ts3_status ts3_norm_create(const ts3_norm_desc *desc, ts3_norm **out);
 ts3_status ts3_norm_free(ts3_norm *h);
 
 /* r may be NULL (y = x); y may be NULL (not wanted) or x or r; out is none of
- * them.  n == 0 is a no-op. */
+ * them.  Any other overlap is refused.  n == 0 is a no-op. */
 ts3_status ts3_norm_forward(ts3_norm *h, const void *x, const void *r, const float *gamma, const float *beta,
                             int64_t n, void *y, void *out, void *stream);
 
 /* Gradients of sum(g * out) + sum(gr * y) for the forward's y: dx [n, C], which
  * is the gradient of x and of r alike, dgamma and dbeta [C] (overwritten).
- * gr may be NULL (zero).  dx may be g or gr.  n == 0 writes zero dgamma and
+ * gr may be NULL (zero).  dx may be g or gr; it overlaps nothing else, nor do
+ * dgamma and dbeta each other.  n == 0 writes zero dgamma and
  * dbeta.  Column sums are in a fixed order for given n. */
 ts3_status ts3_norm_backward(ts3_norm *h, const void *y, const void *g, const void *gr, const float *gamma,
                              int64_t n, void *dx, float *dgamma, float *dbeta, void *stream);

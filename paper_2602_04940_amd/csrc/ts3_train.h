@@ -79,6 +79,17 @@ template <int P, int CP> int gated_point_splits(int nchunk, int64_t points) {
 
 constexpr int64_t GATED_TILE_MAX = 1 << 24;
 
+// Bytes that a call reads or writes.
+struct Range {
+    const void *p;
+    int64_t bytes;
+};
+bool overlap(const Range &a, const Range &b) {
+    const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
+    return a.p && b.p && pa < pb + (uintptr_t)b.bytes && pb < pa + (uintptr_t)a.bytes;
+}
+// Overlaps that are not the same array.
+bool overlap_in_part(const Range &a, const Range &b) { return a.p != b.p && overlap(a, b); }
 bool aligned16(std::initializer_list<const void *> ps) {
     for (const void *p : ps)
         if ((uintptr_t)p & 15) return false;
@@ -220,6 +231,8 @@ ts3_status ts3_gated_forward(ts3_gated *h, const void *x, int64_t n, void *out, 
     if (n == 0) return TS3_OK;
     if (!x || !out || !aligned16({x, out}))
         return fail(TS3_ERR_INVALID_ARG, "x and out must be 16-byte aligned device pointers");
+    const int64_t rows = n * h->desc.C * (h->P == 1 ? 2 : 4);
+    if (overlap_in_part({x, rows}, {out, rows})) return fail(TS3_ERR_INVALID_ARG, "out overlaps x in part");
     return gated_dispatch(h, [&](auto p, auto cp) -> ts3_status {
         constexpr int P = decltype(p)::value, CP = decltype(cp)::value;
         using T = typename GatedIO<P>::T;
@@ -266,8 +279,16 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
         if ((uintptr_t)p & type) return fail(TS3_ERR_INVALID_ARG, "a gradient is not aligned to its type");
     if (n > 0 && (!x || !g || !dx || !aligned16({x, g, dx})))
         return fail(TS3_ERR_INVALID_ARG, "x, g and dx must be 16-byte aligned device pointers");
-    if (n > 0 && (dx == x || dx == g))
-        return fail(TS3_ERR_INVALID_ARG, "dx may not be x or g (the weight gradients read them after dx is written)");
+    // dx is written while other points' x and g are read, the gradients at the end.
+    const int64_t e = h->P == 1 ? 2 : 4, C = h->desc.C, F = h->desc.F;
+    const Range dxr{n > 0 ? dx : nullptr, n * C * e};
+    if (overlap(dxr, {x, dxr.bytes}) || overlap(dxr, {g, dxr.bytes}))
+        return fail(TS3_ERR_INVALID_ARG, "dx may not overlap x or g (the weight gradients read them after dx is written)");
+    const Range outs[] = {dxr, {gr->dWg, C * F * e}, {gr->dWu, C * F * e}, {gr->dWd, C * F * e}, {gr->dbg, F * e},
+                          {gr->dbu, F * e}, {gr->dbd, C * e}};
+    for (const Range &a : outs)
+        for (const Range &b : outs)
+            if (&a < &b && overlap(a, b)) return fail(TS3_ERR_INVALID_ARG, "dx and the gradients may not overlap one another");
     return gated_dispatch(h, [&](auto p, auto cp) -> ts3_status {
         constexpr int P = decltype(p)::value, CP = decltype(cp)::value;
         using T = typename GatedIO<P>::T;
@@ -378,7 +399,15 @@ ts3_status ts3_norm_forward(ts3_norm *h, const void *x, const void *r, const flo
     if (n == 0) return TS3_OK;
     if (!x || !gamma || !beta || !out) return fail(TS3_ERR_INVALID_ARG, "x, gamma, beta or out is NULL");
     if (!aligned16({x, r, y, out})) return fail(TS3_ERR_INVALID_ARG, "x, r, y and out must be 16-byte aligned");
-    if (out == x || out == r || out == y) return fail(TS3_ERR_INVALID_ARG, "out may not be x, r or y");
+    const int64_t rows = n * h->desc.C * (h->desc.io_dtype == TS3_BF16 ? 2 : 4), row = (int64_t)h->desc.C * 4;
+    const Range yr{y, rows}, outr{out, rows};
+    for (const void *p : {x, r, (const void *)y})
+        if (overlap(outr, {p, rows})) return fail(TS3_ERR_INVALID_ARG, "out may not overlap x, r or y");
+    for (const void *p : {x, r})
+        if (overlap_in_part(yr, {p, rows})) return fail(TS3_ERR_INVALID_ARG, "y overlaps x or r in part");
+    for (const float *p : {gamma, beta})
+        if (overlap(outr, {p, row}) || overlap(yr, {p, row}))
+            return fail(TS3_ERR_INVALID_ARG, "y and out may not overlap gamma or beta");
     const auto launch = h->desc.io_dtype == TS3_BF16 ? &launch_norm_fwd<bf16_t> : &launch_norm_fwd<float>;
     launch(h->desc, x, r, gamma, beta, n, y, out, (hipStream_t)stream);
     LAUNCH_CHECK("norm forward");
@@ -392,7 +421,14 @@ ts3_status ts3_norm_backward(ts3_norm *h, const void *y, const void *g, const vo
     if (!dgamma || !dbeta) return fail(TS3_ERR_INVALID_ARG, "dgamma or dbeta is NULL");
     if (n > 0 && (!y || !g || !gamma || !dx)) return fail(TS3_ERR_INVALID_ARG, "y, g, gamma or dx is NULL");
     if (!aligned16({y, g, gr, dx})) return fail(TS3_ERR_INVALID_ARG, "y, g, gr and dx must be 16-byte aligned");
-    if (n > 0 && dx == y) return fail(TS3_ERR_INVALID_ARG, "dx may not be y");
+    const int64_t rows = n * h->desc.C * (h->desc.io_dtype == TS3_BF16 ? 2 : 4), row = (int64_t)h->desc.C * 4;
+    const Range dxr{n > 0 ? dx : nullptr, rows};
+    if (overlap(dxr, {y, rows})) return fail(TS3_ERR_INVALID_ARG, "dx may not overlap y");
+    if (overlap_in_part(dxr, {g, rows}) || overlap_in_part(dxr, {gr, rows}))
+        return fail(TS3_ERR_INVALID_ARG, "dx overlaps g or gr in part");
+    if (overlap(dxr, {gamma, row}) || overlap(dxr, {dgamma, row}) || overlap(dxr, {dbeta, row}) ||
+        overlap({dgamma, row}, {dbeta, row}))
+        return fail(TS3_ERR_INVALID_ARG, "dx may not overlap gamma, dgamma or dbeta, nor these two each other");
     const auto launch = h->desc.io_dtype == TS3_BF16 ? &launch_norm_bwd<bf16_t> : &launch_norm_bwd<float>;
     const int blocks = launch(h->desc, y, g, gr, gamma, n, dx, h->part, (hipStream_t)stream);
     LAUNCH_CHECK("norm backward");

@@ -577,3 +577,66 @@ def test_a_capture_that_would_allocate_is_refused(dtype):
         dx2, grads2 = ff.backward(xt, gt)
         torch.cuda.synchronize()
         assert torch.equal(dx, dx2) and all(torch.equal(grads[n], grads2[n]) for n in NAMES)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_arrays_that_overlap_in_part_are_refused(dtype):
+    """Rows that one workgroup writes while another still reads them: out and dx shifted by a row
+    against their inputs either way, and by their last row alone; gradients on top of each other."""
+    import torch
+    from paper_2602_04940_amd import ResidualNorm
+    from paper_2602_04940_amd import _lib as L
+    C, F, N = 64, 48, 300
+    _, w, _ = _gated(1, C, F, dtype, True)
+    with _operator(C, F, "silu", dtype, w) as ff, ResidualNorm(C, dtype) as norm:
+        buf = torch.zeros((3 * N, C), device="cuda", dtype=ff.torch_dtype)
+        x, far = buf[100:100 + N], torch.zeros((N, C), device="cuda", dtype=ff.torch_dtype)
+        gm = torch.ones(C, device="cuda")
+
+        def refused(call):
+            with pytest.raises(L.TS3Error) as e:
+                call()
+            assert e.value.status == L.TS3_ERR_INVALID_ARG
+        for at in (99, 101, 100 + N - 1):
+            other = buf[at:at + N]
+            for call in (lambda: ff.forward(x, out=other), lambda: ff.backward(x, far, dx=other),
+                         lambda: ff.backward(far, x, dx=other), lambda: norm.forward(x, gm, gm, y=other),
+                         lambda: norm.forward(far, gm, gm, residual=x, y=other), lambda: norm.forward(x, gm, gm, out=other),
+                         lambda: norm.forward(far, gm, gm, residual=x, out=other),
+                         lambda: norm.forward(far, gm, gm, y=x, out=other), lambda: norm.backward(x, far, gm, dx=other),
+                         lambda: norm.backward(far, x, gm, dx=other),
+                         lambda: norm.backward(far, far.clone(), gm, residual_grad=x, dx=other)):
+                refused(call)
+        # next to each other is not on top of each other
+        ff.forward(buf[:N], out=buf[N:2 * N])
+        norm.forward(buf[:N], gm, gm, out=buf[N:2 * N])
+        norm.backward(buf[:N], far, gm, dx=buf[N:2 * N])
+        # C calls: gradients that share their last and first bytes, parameters below the rows
+        lib, stream = L.lib(), None
+        flat = torch.zeros(8 * C * F, device="cuda", dtype=ff.torch_dtype)
+        e = flat.element_size()
+        sizes = dict(dWg=C * F, dWu=C * F, dWd=C * F, dbg=F, dbu=F, dbd=C)
+        names, at, ptrs = list(sizes), flat.data_ptr(), {}
+        for k in names:
+            ptrs[k] = at
+            at += sizes[k] * e
+        dx = torch.empty_like(far)
+        held = dx.nbytes
+        for a, b in [(i, j) for i in names for j in names if i < j]:
+            grads = L.GatedGrads(**{**ptrs, b: ptrs[a] + (sizes[a] - 1) * e})
+            assert lib.ts3_gated_backward(ff.h, x.data_ptr(), far.data_ptr(), N, N, dx.data_ptr(), L.ct.byref(grads),
+                                          stream) == L.TS3_ERR_INVALID_ARG, (a, b)
+        for k in names:
+            grads = L.GatedGrads(**{**ptrs, k: dx.data_ptr() + held - e})
+            assert lib.ts3_gated_backward(ff.h, x.data_ptr(), far.data_ptr(), N, N, dx.data_ptr(), L.ct.byref(grads),
+                                          stream) == L.TS3_ERR_INVALID_ARG, k
+        params = torch.zeros((3, C), device="cuda")
+        p = params.data_ptr()
+        row = 4 * C
+        for dgamma, dbeta in ((p, p + row - 4), (dx.data_ptr(), p), (p, dx.data_ptr() + held - 4)):
+            assert lib.ts3_norm_backward(norm.h, x.data_ptr(), far.data_ptr(), None, gm.data_ptr(), N, dx.data_ptr(), dgamma,
+                                         dbeta, stream) == L.TS3_ERR_INVALID_ARG
+        for gamma, beta in ((dx.data_ptr(), p), (p, dx.data_ptr() + held - 4)):
+            assert lib.ts3_norm_forward(norm.h, x.data_ptr(), None, gamma, beta, N, None, dx.data_ptr(),
+                                        stream) == L.TS3_ERR_INVALID_ARG
+        torch.cuda.synchronize()
