@@ -466,7 +466,8 @@ ts3_status ts3_norm_backward(ts3_norm *h, const void *y, const void *g, const vo
  * Squares and sums are float64.  Each src is a device array of n >= 0 elements
  * aligned to its type; dst is another of the same size, or src itself (in
  * place: left untouched where norm <= max_norm).  No dst may overlap another
- * tensor's src.  `norm` (device float, may be NULL) receives the norm before
+ * tensor's src or dst, nor its own src in part (INVALID_ARG; in place with an
+ * infinite max_norm nothing is written, and tensors may repeat).  `norm` (device float, may be NULL) receives the norm before
  * clipping.  max_norm > 0; +infinity only measures (and copies).  An infinite
  * norm scales by zero (infinite elements become NaN), a NaN norm by one: the
  * caller reads `norm` to skip such a step. */

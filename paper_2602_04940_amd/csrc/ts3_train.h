@@ -147,7 +147,35 @@ struct ClipRun {
     char *dst;
     int64_t n;
     int32_t dtype;
+    int64_t bytes() const { return n * (dtype == TS3_BF16 ? 2 : 4); }
 };
+
+// Whether a written array shares a byte with another read or written one: such elements would be scaled
+// twice, or not at all, by what the workgroups come to first.
+bool clip_overlaps(const std::vector<ClipRun> &runs, bool writes_in_place) {
+    struct Access {
+        uintptr_t a, e;
+        bool write;
+    };
+    std::vector<Access> acc;
+    acc.reserve(2 * runs.size());
+    auto add = [&](const void *p, const ClipRun &r, bool write) {
+        acc.push_back(Access{(uintptr_t)p, (uintptr_t)p + (uintptr_t)r.bytes(), write});
+    };
+    for (const ClipRun &r : runs) {
+        if (r.src != r.dst) add(r.src, r, false);
+        add(r.dst, r, r.src != r.dst || writes_in_place);
+    }
+    auto before = [](const Access &x, const Access &y) { return x.a < y.a; };
+    if (!std::is_sorted(acc.begin(), acc.end(), before)) std::sort(acc.begin(), acc.end(), before);
+    uintptr_t any = 0, written = 0;  // ends of what came so far
+    for (const Access &x : acc) {
+        if (x.a < (x.write ? any : written)) return true;
+        any = std::max(any, x.e);
+        if (x.write) written = std::max(written, x.e);
+    }
+    return false;
+}
 
 }  // namespace
 
@@ -497,6 +525,8 @@ ts3_status ts3_clip_gradients(ts3_clip *h, const ts3_clip_tensor *tensors, int32
             last[t.dtype] = (int)runs.size();
             runs.push_back(ClipRun{(const char *)t.src, (char *)t.dst, t.n, t.dtype});
         }
+        if (clip_overlaps(runs, !std::isinf(max_norm)))
+            return fail(TS3_ERR_INVALID_ARG, "a destination overlaps another tensor (the same one twice, or views of one array)");
         // A multiple of 8 elements, so that pieces keep their tensor's alignment.
         const int64_t piece = std::max(CLIP_PIECE, (total + CLIP_PIECES - 1) / CLIP_PIECES / 8 * 8 + 8);
         std::vector<ClipBatch> batches;

@@ -224,7 +224,8 @@ class GradClip(_Handle):
 
     def __call__(self, grads, max_norm: float, out=None):
         """grads, a list: in place, or into the tensors of the list `out`, one of the same size and
-        type for each."""
+        type for each.  No tensor may come twice or share memory with another, as those of tied
+        parameters would: pass it once."""
         table, device = self._table(grads, out)
         norm = torch.empty((), device="cuda" if device < 0 else device, dtype=torch.float32)
         L.check(L.lib().ts3_clip_gradients(self.h, table, len(grads), max_norm, norm.data_ptr(), _stream(norm)),

@@ -640,3 +640,52 @@ def test_arrays_that_overlap_in_part_are_refused(dtype):
             assert lib.ts3_norm_forward(norm.h, x.data_ptr(), None, gamma, beta, N, None, dx.data_ptr(),
                                         stream) == L.TS3_ERR_INVALID_ARG
         torch.cuda.synchronize()
+
+
+def test_clip_refuses_tensors_that_overlap():
+    """What is written may be no other tensor's: the same one twice, views of one buffer, a
+    destination on another's source or a few elements off its own, in whatever order they come."""
+    import torch
+    from paper_2602_04940_amd import GradClip
+    from paper_2602_04940_amd import _lib as L
+    buf, other = torch.ones(1000, device="cuda"), torch.ones(1000, device="cuda")
+    halves = buf.view(torch.bfloat16)
+    with GradClip() as clip:
+        for grads, out in (([buf, other, buf], None), ([buf[:500], other, buf[499:]], None), ([buf[499:], buf[:500]], None),
+                           ([buf, buf[10:20]], None), ([buf[10:20], other, buf], None), ([buf[:100], halves[199:300]], None),
+                           ([buf[:900]], [buf[100:]]), ([buf[100:]], [buf[:900]]), ([buf, other], [other, buf]),
+                           ([buf[:500], buf[500:]], [other[:500], buf[:500]]), ([buf, other[:10]], [other, torch.zeros(10, device="cuda")]),
+                           ([buf[:10], buf[20:30]], [other[:10], other[9:19]])):
+            with pytest.raises(L.TS3Error) as e:
+                clip(grads, 1.0, out=out)
+            assert e.value.status == L.TS3_ERR_INVALID_ARG
+        torch.cuda.synchronize()
+        assert (buf == 1).all() and (other == 1).all()
+        # not on top of each other; the same source read twice; measured only
+        clip([buf[500:], other, buf[:500]], 1e9)
+        outs = [torch.empty_like(buf) for _ in range(2)]
+        assert abs(float(clip([buf, buf], 1.0, out=outs)) - math.sqrt(2000)) < 1e-4
+        assert torch.equal(outs[0], outs[1]) and float(outs[0][0]) < 0.03
+        assert abs(float(clip([buf, buf], float("inf"))) - math.sqrt(2000)) < 1e-4
+        torch.cuda.synchronize()
+        assert (buf == 1).all()
+
+
+def test_clip_of_many_separate_tensors():
+    """Separate allocations in an order that is not that of their addresses, in place: several
+    launches' worth, as a program's own list of gradients is."""
+    import torch
+    from oracle import train as T
+    from paper_2602_04940_amd import GradClip
+    rng = np.random.default_rng(11)
+    tensors = [torch.from_numpy(rng.standard_normal(int(n)).astype(np.float32)).to("cuda", torch.bfloat16 if i % 3 else torch.float32)
+               for i, n in enumerate(rng.integers(1, 5000, 300))]
+    grads = [tensors[i] for i in rng.permutation(len(tensors))]
+    ref_norm, ref = T.clip([to_host(t) for t in grads], 2.0)
+    with GradClip() as clip:
+        norm = clip(grads, 2.0)
+        torch.cuda.synchronize()
+    assert abs(float(norm) - ref_norm) <= 2.0 ** -23 * ref_norm
+    for t, r in zip(grads, ref):
+        tol = 2.0 ** -22 if t.dtype == torch.float32 else 2.0 ** -8
+        assert np.abs(to_host(t) - r).max() <= tol * np.abs(r).max()
