@@ -13,13 +13,10 @@ from .layer import _DTYPES
 _ACTIVATIONS = {"silu": L.TS3_SILU, "gelu": L.TS3_GELU}
 
 
-# The current stream of a tensor's device, as an integer, without building a Stream object
-# (a microsecond of a call of ten).
+# The current stream of a device, as an integer, without building a Stream object (a microsecond
+# of a call of ten), and the current device.
 _raw_stream = torch._C._cuda_getCurrentRawStream
-
-
-def _stream(t):
-    return _raw_stream(t.device.index)
+_current_device = torch._C._cuda_getDevice
 
 
 def _ptr(t):
@@ -27,10 +24,27 @@ def _ptr(t):
 
 
 class _Handle:
-    """Owns a library object: self.h, released by ts3_<kind>_free."""
+    """Owns a library object: self.h, released by ts3_<kind>_free.  It lives on the device that was
+    current when it was made, where its calls run and its tensors have to be."""
 
     _free = None
     h = None
+
+    def _create(self, *desc):
+        h = ct.c_void_p()
+        create = self._free.replace("_free", "_create")
+        L.check(getattr(L.lib(), create)(*desc, ct.byref(h)), create)
+        self.h, self.device = h, _current_device()
+
+    def _call(self, name, *args):
+        """The library's function on the handle and the current stream of its device."""
+        call = getattr(L.lib(), name)
+        if _current_device() == self.device:  # the library launches on the current device
+            status = call(self.h, *args, _raw_stream(self.device))
+        else:
+            with torch.cuda.device(self.device):
+                status = call(self.h, *args, _raw_stream(self.device))
+        L.check(status, name)
 
     def close(self):
         if self.h:
@@ -50,17 +64,17 @@ class _Handle:
         self.close()
 
     def _rows(self, t, name, n=None):
-        """Checks that t is [n, C] of the operator's type; returns n."""
+        """Checks that t is [n, C] of the operator's type and on its device; returns n."""
         shape = t.shape
-        if not (t.is_cuda and t.dtype is self.torch_dtype and len(shape) == 2 and shape[1] == self.C
+        if not (t.get_device() == self.device and t.dtype is self.torch_dtype and len(shape) == 2 and shape[1] == self.C
                 and (n is None or shape[0] == n) and t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous cuda {self.torch_dtype} tensor "
-                             f"[{'n' if n is None else n}, {self.C}]")
+                             f"[{'n' if n is None else n}, {self.C}] on cuda:{self.device}")
         return shape[0]
 
     def _vector(self, t, name):
-        if not (t.is_cuda and t.dtype is torch.float32 and t.is_contiguous() and t.shape == (self.C,)):
-            raise ValueError(f"{name} must be a contiguous cuda float32 tensor [{self.C}]")
+        if not (t.get_device() == self.device and t.dtype is torch.float32 and t.is_contiguous() and t.shape == (self.C,)):
+            raise ValueError(f"{name} must be a contiguous cuda float32 tensor [{self.C}] on cuda:{self.device}")
 
 
 class GatedWeights:
@@ -96,9 +110,7 @@ class GatedFeedForward(_Handle):
         self.C, self.F = C, F
         code, self.torch_dtype = _DTYPES[dtype]
         self.desc = L.GatedDesc(C=C, F=F, activation=_ACTIVATIONS[activation], io_dtype=code)
-        h = ct.c_void_p()
-        L.check(L.lib().ts3_gated_create(ct.byref(self.desc), ct.byref(h)), "ts3_gated_create")
-        self.h = h
+        self._create(ct.byref(self.desc))
 
     def bytes(self) -> int:
         b = ct.c_int64()
@@ -113,8 +125,10 @@ class GatedFeedForward(_Handle):
         if (w.C, w.F, w.torch_dtype) != (self.C, self.F, self.torch_dtype):
             raise ValueError(f"weights of C={w.C}, F={w.F}, {w.torch_dtype} for an operator of C={self.C}, F={self.F}, "
                              f"{self.torch_dtype}")
+        if any(t is not None and t.get_device() != self.device for t in w.t.values()):
+            raise ValueError(f"the weights must be on cuda:{self.device}")
         s = L.GatedWeights(**{n: (t.data_ptr() if t is not None else None) for n, t in w.t.items()})
-        L.check(L.lib().ts3_gated_load(self.h, ct.byref(s), _stream(w.t["Wg"])), "ts3_gated_load")
+        self._call("ts3_gated_load", ct.byref(s))
 
     def forward(self, x, out=None):
         n = self._rows(x, "x")
@@ -122,7 +136,7 @@ class GatedFeedForward(_Handle):
             out = torch.empty_like(x)
         else:
             self._rows(out, "out", n)
-        L.check(L.lib().ts3_gated_forward(self.h, x.data_ptr(), n, out.data_ptr(), _stream(x)), "ts3_gated_forward")
+        self._call("ts3_gated_forward", x.data_ptr(), n, out.data_ptr())
         return out
 
     def backward(self, x, g, tile: int | None = None, dx=None):
@@ -149,8 +163,7 @@ class GatedFeedForward(_Handle):
             grads[name] = flat[at:at + size].view(shape)
             at += size
         gs = L.GatedGrads(**{k: t.data_ptr() for k, t in grads.items()})
-        L.check(L.lib().ts3_gated_backward(self.h, x.data_ptr(), g.data_ptr(), n, tile, dx.data_ptr(), ct.byref(gs),
-                                           _stream(x)), "ts3_gated_backward")
+        self._call("ts3_gated_backward", x.data_ptr(), g.data_ptr(), n, tile, dx.data_ptr(), ct.byref(gs))
         return dx, grads
 
 
@@ -163,9 +176,7 @@ class ResidualNorm(_Handle):
         self.C = C
         code, self.torch_dtype = _DTYPES[dtype]
         self.desc = L.NormDesc(C=C, io_dtype=code, eps=eps)
-        h = ct.c_void_p()
-        L.check(L.lib().ts3_norm_create(ct.byref(self.desc), ct.byref(h)), "ts3_norm_create")
-        self.h = h
+        self._create(ct.byref(self.desc))
 
     def forward(self, x, gamma, beta, residual=None, y=None, out=None):
         """(y, LayerNorm of y).  Without a residual, y is x itself unless a tensor is given for it."""
@@ -182,8 +193,8 @@ class ResidualNorm(_Handle):
             out = torch.empty_like(x)
         else:
             self._rows(out, "out", n)
-        L.check(L.lib().ts3_norm_forward(self.h, x.data_ptr(), _ptr(residual), gamma.data_ptr(), beta.data_ptr(), n,
-                                         _ptr(y), out.data_ptr(), _stream(x)), "ts3_norm_forward")
+        self._call("ts3_norm_forward", x.data_ptr(), _ptr(residual), gamma.data_ptr(), beta.data_ptr(), n, _ptr(y),
+                   out.data_ptr())
         return (x if y is None else y), out
 
     def backward(self, y, g, gamma, residual_grad=None, dx=None):
@@ -200,9 +211,8 @@ class ResidualNorm(_Handle):
             self._rows(dx, "dx", n)
         d = torch.empty((2, self.C), device=y.device, dtype=torch.float32)
         dgamma, dbeta = d.unbind()
-        L.check(L.lib().ts3_norm_backward(self.h, y.data_ptr(), g.data_ptr(), _ptr(residual_grad), gamma.data_ptr(), n,
-                                          dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), _stream(y)),
-                "ts3_norm_backward")
+        self._call("ts3_norm_backward", y.data_ptr(), g.data_ptr(), _ptr(residual_grad), gamma.data_ptr(), n,
+                   dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr())
         return dx, dgamma, dbeta
 
 
@@ -218,16 +228,15 @@ class GradClip(_Handle):
         except ImportError as e:
             raise RuntimeError("_tensors.so is missing or unusable: build it with __graft_entry__.build()") from e
         self._table = _tensors.clip_table
-        h = ct.c_void_p()
-        L.check(L.lib().ts3_clip_create(ct.byref(h)), "ts3_clip_create")
-        self.h = h
+        self._create()
 
     def __call__(self, grads, max_norm: float, out=None):
         """grads, a list: in place, or into the tensors of the list `out`, one of the same size and
         type for each.  No tensor may come twice or share memory with another, as those of tied
         parameters would: pass it once."""
         table, device = self._table(grads, out)
-        norm = torch.empty((), device="cuda" if device < 0 else device, dtype=torch.float32)
-        L.check(L.lib().ts3_clip_gradients(self.h, table, len(grads), max_norm, norm.data_ptr(), _stream(norm)),
-                "ts3_clip_gradients")
+        if device >= 0 and device != self.device:
+            raise ValueError(f"gradients must be on cuda:{self.device}, where the GradClip was made")
+        norm = torch.empty((), device=self.device, dtype=torch.float32)
+        self._call("ts3_clip_gradients", table, len(grads), max_norm, norm.data_ptr())
         return norm
