@@ -6,6 +6,7 @@ import os
 import shutil
 import subprocess
 import sysconfig
+import warnings
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(PKG, "csrc", "ts3.hip")
@@ -31,27 +32,48 @@ def tensors_command(out: str) -> list[str]:
     """Host code against this Python and this torch: their headers, and torch's libraries by path."""
     import torch
     from torch.utils import cpp_extension
+    gxx = shutil.which("g++")
+    if not gxx:
+        raise RuntimeError("g++ not found")
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     include = [sysconfig.get_paths()["include"], *cpp_extension.include_paths()]
-    return [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared",
+    return [gxx, "-O2", "-std=c++17", "-fPIC", "-shared",
             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *["-I" + p for p in include], "-o", out,
             TENSORS_SRC, "-L" + libs, "-Wl,-rpath," + libs, "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
+def _start(cmd):
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def _finish(cmd, job, verbose):
+    """Waits for a compiler; raises with its output if it failed."""
+    out = job.communicate()[0]
+    msgs = "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l)
+    if job.returncode != 0:
+        raise RuntimeError(f"{os.path.basename(cmd[0])} failed ({job.returncode}):\n{' '.join(cmd)}\n{msgs}")
+    if verbose and msgs.strip():
+        print(msgs)
+
+
 def build_library(verbose: bool = False) -> str:
-    """Always recompiles both; writes to temporary names and renames on success."""
+    """Always recompiles both, side by side; writes to temporary names and renames on success.  The
+    library needs hipcc alone.  Where the tensor-table module, which GradClip reads its lists with,
+    cannot be built, an older one is removed and a warning says so: the rest works without it."""
     tmp, tensors_tmp = LIB + ".tmp", TENSORS + ".tmp"
-    cmds = [[hipcc(), *HIP_FLAGS, "-o", tmp, SRC], tensors_command(tensors_tmp)]
-    jobs = [subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) for c in cmds]
-    outs = [j.communicate()[0] for j in jobs]
-    for cmd, job, out in zip(cmds, jobs, outs):
-        msgs = "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l)
-        if job.returncode != 0:
-            raise RuntimeError(f"{os.path.basename(cmd[0])} failed ({job.returncode}):\n{' '.join(cmd)}\n{msgs}")
-        if verbose and msgs.strip():
-            print(msgs)
+    cmd = [hipcc(), *HIP_FLAGS, "-o", tmp, SRC]
+    job = _start(cmd)
+    try:
+        tensors_cmd = tensors_command(tensors_tmp)
+        _finish(tensors_cmd, _start(tensors_cmd), verbose)
+        os.replace(tensors_tmp, TENSORS)
+    except Exception as e:
+        if os.path.exists(TENSORS):
+            os.remove(TENSORS)
+        warnings.warn(f"{os.path.basename(TENSORS)} could not be built, GradClip will not work: {e}")
+    finally:
+        _finish(cmd, job, verbose)
     os.replace(tmp, LIB)
-    os.replace(tensors_tmp, TENSORS)
     return LIB
 
 
