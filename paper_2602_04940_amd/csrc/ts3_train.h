@@ -4,6 +4,7 @@
 #pragma once
 #include "ts3_clip.h"
 #include "ts3_gated.h"
+#include "ts3_gated_rules.h"
 #include "ts3_norm.h"
 
 struct ts3_gated {
@@ -39,42 +40,6 @@ template <typename F> auto gated_dispatch(const ts3_gated *h, F fn) {
         }
     };
     return h->P == 1 ? with(ic<1>{}) : with(ic<3>{});
-}
-
-// Splits of the hidden units over workgroups, for a call of n points in nb blocks that leaves
-// compute units idle.  S splits take chunks / S steps of t us (what one workgroup alone on its
-// compute unit takes: 0.5 us and 5 ns per channel, 18 in float32), and write and read S sums of
-// n CP floats at 1.9 TB/s together: the sum of both is least at S = sqrt(chunks t / sums).
-int gated_splits(int64_t n, int64_t nb, int nchunk, int P, int CP) {
-    const double t = 0.5 + (P == 1 ? 0.005 : 0.018) * CP, sums = (double)n * CP * 4 / 1.9e6;
-    const int64_t best = (int64_t)std::ceil(std::sqrt(nchunk * t / sums));
-    const int64_t s = std::max<int64_t>(1, std::min(std::min<int64_t>(best, nchunk), device_cu_count() / std::max<int64_t>(nb, 1)));
-    const int per = (int)((nchunk + s - 1) / s);
-    return (nchunk + per - 1) / per;
-}
-
-// Waves of the weight gradients' workgroups: eight where they cover the hidden units with no more
-// than an eighth of their products on units that do not exist.
-template <int P, int CP> int gated_dw_waves(int nchunk) {
-    if constexpr (GatedDwWide<P, CP>::USE8) {
-        constexpr int HB = GatedDw<P, CP, 8>::HB;
-        const int F = nchunk * 32, covered = (F + HB - 1) / HB * HB;
-        if (8 * (covered - F) <= covered) return 8;
-    }
-    return 4;
-}
-
-// Splits of the points for the weight gradients: at most eight waves per compute unit in all.  A
-// split costs its sums, 3 F C floats written and read at 2.5 TB/s together, and saves
-// steps of KP points (0.6 us each, 0.8 in float32), so few points take fewer: of 3,000 at C =
-// 256, F = 1024 in bfloat16, 21 splits took 34 us with their sums, 7 take 22.
-template <int P, int CP> int gated_point_splits(int nchunk, int64_t points) {
-    using Dw = GatedDw<P, CP, 4>;
-    const int W = gated_dw_waves<P, CP>(nchunk), HB = Dw::HB / 4 * W;
-    const int nhb = (nchunk * 32 + HB - 1) / HB;
-    const int64_t most = std::max<int64_t>(1, (int64_t)(8 / W) * device_cu_count() / (3 * nhb));
-    const double steps = (double)points / Dw::KP * (P == 1 ? 0.6 : 0.8), sums = 3.0 * nchunk * 32 * CP * 4 / 2.5e6;
-    return (int)std::min<int64_t>(most, std::max<int64_t>(1, (int64_t)std::ceil(std::sqrt(steps / sums))));
 }
 
 constexpr int64_t GATED_TILE_MAX = 1 << 24;
@@ -265,11 +230,11 @@ ts3_status ts3_gated_forward(ts3_gated *h, const void *x, int64_t n, void *out, 
         constexpr int P = decltype(p)::value, CP = decltype(cp)::value;
         using T = typename GatedIO<P>::T;
         constexpr int PTS = GatedShape<P, CP>::PTS;
-        const int C = h->desc.C;
+        const int C = h->desc.C, cus = device_cu_count();
         hipStream_t st = (hipStream_t)stream;
         for (int64_t p0 = 0; p0 < n; p0 += MAX_WGS * PTS) {
             const int64_t m = std::min<int64_t>(n - p0, MAX_WGS * PTS), nb = (m + PTS - 1) / PTS;
-            const int S = gated_splits(m, nb, h->nchunk, P, CP), per = (h->nchunk + S - 1) / S;
+            const int S = gated_splits(m, nb, h->nchunk, P, CP, cus), per = (h->nchunk + S - 1) / S;
             T *const to = (T *)out + p0 * C;
             const bool silu = h->desc.activation == TS3_SILU;
             auto launch = [&](auto hw) {
@@ -278,9 +243,8 @@ ts3_status ts3_gated_forward(ts3_gated *h, const void *x, int64_t n, void *out, 
                 hipLaunchKernelGGL(kernel, dim3((unsigned)(nb * S)), dim3(256 * HW), 0, st, (const T *)x + p0 * C, m, C,
                                    h->ops, h->nchunk, per, S, h->bd, to, h->part);
             };
-            // One workgroup per compute unit or none: two waves per SIMD on the same points.
             if constexpr (GatedShape<P, CP>::OCC == 2)
-                if (per > 1 && nb * S <= device_cu_count()) launch(ic<2>{});
+                if (gated_halves<P, CP>(nb * S, per, cus) == 2) launch(ic<2>{});
                 else launch(ic<1>{});
             else launch(ic<1>{});
             LAUNCH_CHECK("gated forward");
@@ -322,18 +286,18 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
         using T = typename GatedIO<P>::T;
         constexpr bool WIDE = GatedWide<P, CP>::USE;
         constexpr int PTS = WIDE ? GatedWide<P, CP>::PTS : GatedShapeX<P, CP>::PTS;
-        const int C = h->desc.C, F = h->desc.F, nchunk = h->nchunk, FP = nchunk * 32, BW = std::max(FP, CP);
+        const int C = h->desc.C, F = h->desc.F, nchunk = h->nchunk, FP = nchunk * 32, BW = std::max(FP, CP), cus = device_cu_count();
         const int W = gated_dw_waves<P, CP>(nchunk), HB = GatedDw<P, CP, 4>::HB / 4 * W, nhb = (FP + HB - 1) / HB;
         hipStream_t st = (hipStream_t)stream;
         // k_gated_load leaves zeros after the 64 biases of a chunk's block.
         const unsigned char *const zeros = h->ops + GatedOps<P, CP, GatedShape<P, CP>::MT>::BIAS + 256;
         const int64_t step = std::min(std::min(tile, GATED_TILE_MAX), std::max<int64_t>(n, 1));
-        const int SP = n > 0 ? gated_point_splits<P, CP>(nchunk, step) : 0;
+        const int SP = n > 0 ? gated_point_splits<P, CP>(nchunk, step, cus) : 0;
         if (n > 0) {
             // da, du and h of a tile, and in bfloat16 the sums of da and du over 32 points each
             const int64_t rows = (step + PTS - 1) / PTS * PTS;
             const int64_t need = rows * 3 * FP * (int64_t)sizeof(T) + (P == 1 ? rows / 32 * 2 * FP * 4 : 0);
-            const int most = gated_point_splits<P, CP>(nchunk, GATED_TILE_MAX);
+            const int most = gated_point_splits<P, CP>(nchunk, GATED_TILE_MAX, cus);
             const int64_t wbytes = (int64_t)most * 3 * FP * CP * 4, bbytes = (int64_t)most * 3 * BW * 4;
             ts3_status s = h->wpart.reserve(wbytes, st, h->bytes);
             if (s == TS3_OK) s = h->bpart.reserve(bbytes, st, h->bytes);
@@ -344,7 +308,7 @@ ts3_status ts3_gated_backward(ts3_gated *h, const void *x, const void *g, int64_
         float *const wpart = (float *)h->wpart.p, *const bpart = (float *)h->bpart.p;
         for (int64_t t0 = 0; t0 < n; t0 += step) {
             const int64_t m = std::min(step, n - t0), nb = (m + PTS - 1) / PTS, tp = nb * PTS;
-            const int S = gated_splits(m, nb, nchunk, P, CP), per = (nchunk + S - 1) / S;
+            const int S = gated_splits(m, nb, nchunk, P, CP, cus), per = (nchunk + S - 1) / S;
             const T *const xt = (const T *)x + t0 * C, *const gt = (const T *)g + t0 * C;
             T *const dxt = (T *)dx + t0 * C;
             const bool silu = h->desc.activation == TS3_SILU;

@@ -14,6 +14,7 @@ import math
 import numpy as np
 import pytest
 
+from gated_shapes import LONG, MIDDLE
 from gpu_helpers import banner, normwise, rel_l2, row_rel, to_device, to_host
 
 pytestmark = pytest.mark.gpu
@@ -689,3 +690,27 @@ def test_clip_of_many_separate_tensors():
     for t, r in zip(grads, ref):
         tol = 2.0 ** -22 if t.dtype == torch.float32 else 2.0 ** -8
         assert np.abs(to_host(t) - r).max() <= tol * np.abs(r).max()
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("N,C,F,tile", LONG)
+def test_gated_long_loops(N, C, F, tile, dtype, kind):
+    test_gated_forward_and_backward(N, C, F, tile, dtype, kind)
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("N,C,F", MIDDLE)
+def test_gated_forward_of_a_workgroup_per_compute_unit(N, C, F, dtype, kind):
+    import torch
+    from oracle import train as T
+    banner(f"gated forward N={N} C={C} F={F} {dtype} {kind}")
+    x, w, _ = _gated(N, C, F, dtype, True)
+    with _operator(C, F, kind, dtype, w) as ff:
+        xt = to_device(x, dtype)
+        out = ff.forward(xt)
+        ff.forward(xt, out=xt)
+        torch.cuda.synchronize()
+    _check("out", out, T.gated_forward(x, w, kind), dtype, (C, F))
+    assert torch.equal(xt, out)
