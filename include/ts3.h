@@ -400,8 +400,9 @@ typedef struct {
 
 typedef struct ts3_gated ts3_gated; /* opaque */
 
-/* Device bytes held from the start: the operands (about 6 C F elements, three
- * times that many for float32) and up to 68 MB of partial sums. */
+/* Device bytes held from the start: the operands (6 C F bfloat16 elements with C
+ * padded to a multiple of 64 and F to one of 32, three times that many for
+ * float32) and up to 34 MB of partial sums.  The first backward adds its own. */
 ts3_status ts3_gated_create(const ts3_gated_desc *desc, ts3_gated **out);
 ts3_status ts3_gated_free(ts3_gated *h);
 ts3_status ts3_gated_bytes(const ts3_gated *h, int64_t *bytes);

@@ -501,7 +501,7 @@ __global__ __launch_bounds__(256 * HW, (GatedShape<P, CP>::OCC)) void k_gated_fw
         barrier();  // (G, U) of chunk i are read by all; with one slot, D is in LDS
         // The wave that has its vector work before it goes first, or the two of a SIMD share each phase
         // in step and neither's products run beside the other's activation (1M bfloat16 points at
-        // C = 256, F = 1024: 1.39 -> 1.33 ms; the other way round 1.43).
+        // C = 256, F = 1024: SiLU 1.40 -> 1.34 ms, GELU 1.525 -> 1.515; the other way round 1.43).
         __builtin_amdgcn_s_setprio(1);
         if (i + 1 < mine) issue_a(i + 1);
         Parts<P> hf[NP][M::KF];
@@ -803,7 +803,12 @@ __global__ __launch_bounds__(256, (GatedShapeX<P, CP>::OCC)) void k_gated_dx(
 // would have to do all (bfloat16 at CP = 256: 8,900 cycles per chunk, of 2,560 of products;
 // float32 at CP = 128: 350,000 points of F = 512 in 1.53 ms, of 0.68 of products).  There the
 // backward takes two kernels: the slopes without the sums, and dx, which reads da and du back
-// from the store, on two waves per SIMD (float32: 0.88 + 0.47 ms).
+// from the store, on two waves per SIMD (float32: 0.85 + 0.47 ms).  Where one kernel has two waves
+// per SIMD it is faster: a bfloat16 step of 300,000 points at C = 128, F = 512 takes 0.76 ms, in two
+// kernels 0.80, at C = 64, F = 256 0.33 and 0.38.  Float32 rows of more than 128 channels fill 288
+// registers and more beside the 96 of two chunks' results, which k_gated_slopes3 has no room for:
+// they stay with the one kernel and its ring of sections (not tried otherwise; a step of 100,003
+// points at C = 256, F = 683 takes 2.58 ms, at C = 192, F = 512 1.48 ms).
 template <int P, int CP> struct GatedWide {
     static constexpr bool USE = P == 1 ? CP > 128 : CP == 128;
     static constexpr int WAVES = 4, PTS = WAVES * 32;

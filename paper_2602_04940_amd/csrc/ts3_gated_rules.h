@@ -22,7 +22,9 @@ inline int gated_splits(int64_t n, int64_t nb, int nchunk, int P, int CP, int cu
 }
 
 // The forward's HW, for `wgs` workgroups of `per` chunks: one workgroup per compute unit or none takes
-// two waves per SIMD on the same points.
+// two waves per SIMD on the same points.  At C = 256, F = 1024 in bfloat16, with one wave in brackets:
+// 20,000 points 48 us (52.5), 32,768 58 (59); 32,769, on one wave, 62.6.  Of few points in short
+// splits it loses: 4,096 in six splits 28.3 us (26.6), in float32 at C = 128, F = 512 25.2 (23.4).
 template <int P, int CP> int gated_halves(int64_t wgs, int per, int cus) {
     return GatedShape<P, CP>::OCC == 2 && per > 1 && wgs <= cus ? 2 : 1;
 }
