@@ -485,6 +485,139 @@ ts3_status ts3_clip_free(ts3_clip *h);
 ts3_status ts3_clip_gradients(ts3_clip *h, const ts3_clip_tensor *tensors, int32_t count, float max_norm,
                               float *norm, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Operators of a conditioned block: attention from points to the states of an
+ * encoder, the norms around a block with its gate and residual scale, and
+ * orthogonalised updates of a list of weight matrices.  Handles, streams,
+ * devices, captures and workspaces are as for the training operators above. */
+
+/* Attention of B samples' points [N] to B samples' states [S], of another
+ * number, with H query heads of D values; Hkv heads of keys and values, which
+ * divides H, are each shared by H / Hkv query heads in a row:
+ *     s_j = scale q.k_j,  p = softmax(s),  out = sum_j p_j v_j,  lse = log sum_j e^s_j
+ * over the states j that are there: those before the sample's length, and not
+ * masked.  Where none is, out is 0 and lse minus infinity.
+ *  D       : a multiple of 16 up to 128, H up to 1024; beyond: TS3_ERR_UNSUPPORTED.
+ *  io_dtype: ts3_dtype of q, k, v, out and their gradients.  TS3_BF16 computes
+ *            on bf16 matrix cores with float32 sums and rounds p (and, in the
+ *            backward, p and ds) to bfloat16 once; TS3_FP32 keeps every operand to
+ *            float32 precision in three bf16 parts.
+ *  scale   : finite and > 0; 0 stands for 1 / sqrt(D). */
+typedef struct {
+    int32_t H, Hkv, D;
+    int32_t io_dtype;
+    float scale;
+} ts3_cross_desc;
+typedef struct ts3_cross ts3_cross; /* opaque */
+ts3_status ts3_cross_create(const ts3_cross_desc *desc, ts3_cross **out);
+ts3_status ts3_cross_free(ts3_cross *h);
+ts3_status ts3_cross_bytes(const ts3_cross *h, int64_t *bytes);
+
+/* A device array [sample][point or state][head][D] with strides in elements;
+ * the D values of a head lie in a row.  16-byte aligned, strides multiples of
+ * 16 bytes (0, for a shared sample or head, is one). */
+typedef struct {
+    const void *p;
+    int64_t batch, row, head;
+} ts3_view;
+
+/* lengths (device int32 [B], may be NULL: S each; taken as 0 to S where outside)
+ * and mask (device bytes [B][S], 0 = absent, may be NULL) say which states are
+ * there.  What the others hold is of no account, not-a-number included. */
+typedef struct {
+    int32_t B, N, S;
+    ts3_view q, k, v;
+    const int32_t *lengths;
+    const uint8_t *mask;
+} ts3_cross_inputs;
+
+/* out [B][N][H][D], contiguous and 16-byte aligned, lse float [B][H][N]; they
+ * overlap no input (TS3_ERR_INVALID_ARG).  S = 0 is allowed; B = 0 or N = 0 is a
+ * no-op.  TS3_ERR_UNSUPPORTED where N * H / Hkv or S reaches 2^31 - 1024, or a
+ * launch 2^24 workgroups (of 32 to 256 rows).  Few points split the states over
+ * workgroups, whose parts are joined in a fixed order; the parts' workspace grows
+ * with the calls, as the store of ts3_gated_backward does. */
+ts3_status ts3_cross_forward(ts3_cross *h, const ts3_cross_inputs *in, void *out, float *lse, void *stream);
+
+/* Gradients of sum(g * out) for the forward's inputs, out and lse: dq as out, dk
+ * and dv [B][S][Hkv][D], contiguous, 16-byte aligned, overwritten; zero for
+ * absent states.  None overlaps another or an input.  Sums over points are
+ * split and joined in a fixed order.  The workspace (parts, and a float per point
+ * and head) grows with the calls. */
+ts3_status ts3_cross_backward(ts3_cross *h, const ts3_cross_inputs *in, const void *out, const float *lse,
+                              const ts3_view *g, void *dq, void *dk, void *dv, void *stream);
+
+/* The norms around a block, over rows of C values (a multiple of 16 up to 512):
+ *     m = LN(f) gamma_post + beta_post,  y = x + scale * sigmoid(gate) * m
+ *     out = LN(y) gamma_pre + beta_pre
+ * with LN as in ts3_norm, f the block's output, x the residual stream and out what the
+ * next block reads.  f, x, gate, y, out and their gradients are [n, C] of the io
+ * dtype, 16-byte aligned; the parameters [C] and their gradients float32.
+ * Statistics and sums are float32; out is that of the unrounded y. */
+typedef struct {
+    int32_t C;
+    int32_t io_dtype;
+    float eps; /* finite, >= 0; of both norms */
+} ts3_sandwich_desc;
+typedef struct {
+    const float *gamma_post, *beta_post, *scale;
+    const float *gamma_pre, *beta_pre; /* both NULL: no second norm */
+} ts3_sandwich_params;
+typedef struct {
+    float *gamma_post, *beta_post, *scale;
+    float *gamma_pre, *beta_pre; /* both NULL without gn */
+} ts3_sandwich_grads;
+typedef struct ts3_sandwich ts3_sandwich; /* opaque */
+ts3_status ts3_sandwich_create(const ts3_sandwich_desc *desc, ts3_sandwich **out);
+ts3_status ts3_sandwich_free(ts3_sandwich *h);
+
+/* gate may be NULL (a factor of 1); out, gamma_pre and beta_pre are given together
+ * or all NULL.  y may be x; any other overlap is refused.  n == 0 is a no-op. */
+ts3_status ts3_sandwich_forward(ts3_sandwich *h, const void *f, const void *x, const void *gate,
+                                const ts3_sandwich_params *p, int64_t n, void *y, void *out, void *stream);
+
+/* Gradients of sum(gy * y) + sum(gn * out) for the forward's f, y and gate: df,
+ * dx, dgate [n, C] and the parameters' (overwritten).  gy may be NULL (zero); gn
+ * may be NULL (no second norm: y is not read, d->gamma_pre and d->beta_pre are
+ * NULL), but not both.  dgate is given where gate is.  dx may be gy; any other
+ * overlap is refused.  p->beta_pre is not read.  n == 0 writes zero parameter
+ * gradients.  Column sums are in a fixed order for given n. */
+ts3_status ts3_sandwich_backward(ts3_sandwich *h, const void *f, const void *y, const void *gate, const void *gy,
+                                 const void *gn, const ts3_sandwich_params *p, int64_t n, void *df, void *dx,
+                                 void *dgate, const ts3_sandwich_grads *d, void *stream);
+
+/* Orthogonalised updates: every matrix G of a list becomes the result of `steps`
+ * (1 to 64) Newton-Schulz steps from X = G / (|G| + eps), |G| its Frobenius norm:
+ *     X <- a X + (b A + c A A) X,  A = X X^T,  (a, b, c) = (3.4445, -4.7750, 2.0315)
+ * which leaves its singular vectors and moves its singular values near one (the
+ * coefficients are the Muon optimiser's).  The norm is float64, products carry
+ * operands of 22 bits and float32 sums.  A not-a-number or infinity anywhere in a
+ * matrix makes all or part of its result not-a-number; other matrices are not
+ * touched by it.  A zero matrix gives zeros, with eps = 0 not-a-numbers. */
+typedef struct {
+    int32_t steps;
+    float eps; /* finite, >= 0 */
+} ts3_orth_desc;
+/* A tensor of `batch` matrices [rows, cols], each contiguous and one after another.
+ * src and dst device arrays aligned to their type; dst may be src. */
+typedef struct {
+    const void *src;
+    void *dst;
+    int32_t rows, cols, batch;
+    int32_t dtype; /* ts3_dtype */
+} ts3_matrix;
+typedef struct ts3_orth ts3_orth; /* opaque */
+ts3_status ts3_orth_create(const ts3_orth_desc *desc, ts3_orth **out);
+ts3_status ts3_orth_free(ts3_orth *h);
+ts3_status ts3_orth_bytes(const ts3_orth *h, int64_t *bytes);
+
+/* 0 <= count <= 16384 tensors, sides up to 32768 (TS3_ERR_UNSUPPORTED beyond);
+ * an empty tensor is skipped.  No two dst may overlap (INVALID_ARG); a dst may
+ * overlap any src, as every source is read before the first result is written.
+ * The workspace, about 8 (n + s) bytes for n elements and s = min(rows, cols)^2,
+ * all padded to multiples of 64, grows with the calls. */
+ts3_status ts3_orth_matrices(ts3_orth *h, const ts3_matrix *matrices, int32_t count, void *stream);
+
 const char *ts3_status_string(ts3_status s);
 const char *ts3_last_error(void); /* thread-local detail of the last failure */
 

@@ -5,7 +5,7 @@ The layer runs in ``libts3.so`` (HIP kernels behind the C ABI of
 Importing this package loads nothing; the library is loaded on first use.
 """
 __all__ = ["PhysicsAttention", "LayerWeights", "TransolverStack", "BlockWeights", "GatedFeedForward",
-           "GatedWeights", "ResidualNorm", "GradClip"]
+           "GatedWeights", "ResidualNorm", "GradClip", "CrossAttention", "SandwichNorm", "Orthogonalizer"]
 
 
 def __getattr__(name):
@@ -18,4 +18,7 @@ def __getattr__(name):
     if name in ("GatedFeedForward", "GatedWeights", "ResidualNorm", "GradClip"):
         from . import train
         return getattr(train, name)
+    if name in ("CrossAttention", "SandwichNorm", "Orthogonalizer"):
+        from . import conditioned
+        return getattr(conditioned, name)
     raise AttributeError(name)

@@ -71,6 +71,40 @@ class ClipTensor(ct.Structure):
                 ("reserved", ct.c_int32)]
 
 
+class CrossDesc(ct.Structure):
+    _fields_ = [("H", ct.c_int32), ("Hkv", ct.c_int32), ("D", ct.c_int32), ("io_dtype", ct.c_int32), ("scale", ct.c_float)]
+
+
+class View(ct.Structure):
+    _fields_ = [("p", ct.c_void_p), ("batch", ct.c_int64), ("row", ct.c_int64), ("head", ct.c_int64)]
+
+
+class CrossInputs(ct.Structure):
+    _fields_ = [("B", ct.c_int32), ("N", ct.c_int32), ("S", ct.c_int32), ("q", View), ("k", View), ("v", View),
+                ("lengths", ct.c_void_p), ("mask", ct.c_void_p)]
+
+
+class SandwichDesc(ct.Structure):
+    _fields_ = [("C", ct.c_int32), ("io_dtype", ct.c_int32), ("eps", ct.c_float)]
+
+
+SANDWICH_NAMES = ("gamma_post", "beta_post", "scale", "gamma_pre", "beta_pre")
+
+
+class SandwichParams(ct.Structure):
+    """Of the parameters, and of their gradients."""
+    _fields_ = [(n, ct.c_void_p) for n in SANDWICH_NAMES]
+
+
+class OrthDesc(ct.Structure):
+    _fields_ = [("steps", ct.c_int32), ("eps", ct.c_float)]
+
+
+class Matrix(ct.Structure):
+    _fields_ = [("src", ct.c_void_p), ("dst", ct.c_void_p), ("rows", ct.c_int32), ("cols", ct.c_int32),
+                ("batch", ct.c_int32), ("dtype", ct.c_int32)]
+
+
 _P = ct.c_void_p
 # name -> (restype, argtypes); must match include/ts3.h
 SIGNATURES = {
@@ -111,6 +145,19 @@ SIGNATURES = {
     "ts3_clip_create": (ct.c_int, [ct.POINTER(_P)]),
     "ts3_clip_free": (ct.c_int, [_P]),
     "ts3_clip_gradients": (ct.c_int, [_P, _P, ct.c_int32, ct.c_float, _P, _P]),
+    "ts3_cross_create": (ct.c_int, [ct.POINTER(CrossDesc), ct.POINTER(_P)]),
+    "ts3_cross_free": (ct.c_int, [_P]),
+    "ts3_cross_bytes": (ct.c_int, [_P, ct.POINTER(ct.c_int64)]),
+    "ts3_cross_forward": (ct.c_int, [_P, _P, _P, _P, _P]),
+    "ts3_cross_backward": (ct.c_int, [_P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "ts3_sandwich_create": (ct.c_int, [ct.POINTER(SandwichDesc), ct.POINTER(_P)]),
+    "ts3_sandwich_free": (ct.c_int, [_P]),
+    "ts3_sandwich_forward": (ct.c_int, [_P, _P, _P, _P, _P, ct.c_int64, _P, _P, _P]),
+    "ts3_sandwich_backward": (ct.c_int, [_P, _P, _P, _P, _P, _P, _P, ct.c_int64, _P, _P, _P, _P, _P]),
+    "ts3_orth_create": (ct.c_int, [ct.POINTER(OrthDesc), ct.POINTER(_P)]),
+    "ts3_orth_free": (ct.c_int, [_P]),
+    "ts3_orth_bytes": (ct.c_int, [_P, ct.POINTER(ct.c_int64)]),
+    "ts3_orth_matrices": (ct.c_int, [_P, _P, ct.c_int32, _P]),
     "ts3_status_string": (ct.c_char_p, [ct.c_int]),
     "ts3_last_error": (ct.c_char_p, []),
 }

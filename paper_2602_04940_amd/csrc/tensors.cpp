@@ -1,6 +1,6 @@
 // Tables of tensors for the C ABI, for lists too long to be read from Python attribute by
 // attribute (five calls of 40 ns each on hundreds of tensors: 200 us beside 40 us on the GPU).
-// A module of one function, built next to the library; it holds no computation.
+// A module built next to the library; it holds no computation.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -85,7 +85,71 @@ PyObject *clip_table(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     return result;
 }
 
-PyMethodDef methods[] = {{"clip_table", (PyCFunction)(void (*)())clip_table, METH_FASTCALL, "Rows of ts3_clip_tensor."},
+// matrix_table(tensors, out) -> (ts3_matrix rows as bytes, device index or -1)
+PyObject *matrix_table(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    if (nargs != 2) {
+        PyErr_SetString(PyExc_TypeError, "matrix_table(tensors, out)");
+        return nullptr;
+    }
+    PyObject *from = PySequence_Fast(args[0], "tensors must be a sequence of tensors");
+    PyObject *to = from ? PySequence_Fast(args[1], "outputs must be a sequence of tensors") : nullptr;
+    PyObject *rows = nullptr, *result = nullptr;
+    try {
+        const Py_ssize_t count = from ? PySequence_Fast_GET_SIZE(from) : 0;
+        if (to && PySequence_Fast_GET_SIZE(to) != count) {
+            PyErr_Format(PyExc_ValueError, "%zd output tensors expected, not %zd", count, PySequence_Fast_GET_SIZE(to));
+        } else if (to) {
+            rows = PyBytes_FromStringAndSize(nullptr, count * (Py_ssize_t)sizeof(ts3_matrix));
+            ts3_matrix *r = rows ? reinterpret_cast<ts3_matrix *>(PyBytes_AS_STRING(rows)) : nullptr;
+            bool ok = rows != nullptr;
+            int device = -1;
+            for (Py_ssize_t i = 0; ok && i < count; ++i) {
+                PyObject *const a = PySequence_Fast_GET_ITEM(from, i), *const b = PySequence_Fast_GET_ITEM(to, i);
+                const void *dst = nullptr;
+                int64_t n = 0;
+                int32_t dtype = 0;
+                int da = 0, db = 0;
+                ok = read_tensor(a, "a tensor", &r[i].src, &n, &r[i].dtype, &da) && read_tensor(b, "an output", &dst, &n, &dtype, &db);
+                if (!ok) break;
+                const auto shape = THPVariable_Unpack(a).sizes();
+                const char *wrong = nullptr;
+                if (i == 0) device = da;
+                if (da != device || db != device) wrong = "tensors must be on one device";
+                else if (dtype != r[i].dtype || THPVariable_Unpack(b).sizes() != shape)
+                    wrong = "an output tensor must have its tensor's type and shape";
+                else if (shape.size() < 2) wrong = "a tensor must have two dimensions at least";
+                int64_t size[3] = {0, 0, 1};
+                if (!wrong) {
+                    size[0] = shape[shape.size() - 2];
+                    size[1] = shape[shape.size() - 1];
+                    for (size_t k = 0; k + 2 < shape.size(); ++k) size[2] *= shape[k];
+                    for (int64_t s : size)
+                        if (s > INT32_MAX) wrong = "a tensor has a side of 2^31 or more";
+                }
+                if (wrong) {
+                    PyErr_SetString(PyExc_ValueError, wrong);
+                    ok = false;
+                    break;
+                }
+                r[i].dst = const_cast<void *>(dst);
+                r[i].rows = (int32_t)size[0];
+                r[i].cols = (int32_t)size[1];
+                r[i].batch = (int32_t)size[2];
+            }
+            if (ok) result = Py_BuildValue("Oi", rows, device);
+        }
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        result = nullptr;
+    }
+    Py_XDECREF(rows);
+    Py_XDECREF(to);
+    Py_XDECREF(from);
+    return result;
+}
+
+PyMethodDef methods[] = {{"matrix_table", (PyCFunction)(void (*)())matrix_table, METH_FASTCALL, "Rows of ts3_matrix."},
+                         {"clip_table", (PyCFunction)(void (*)())clip_table, METH_FASTCALL, "Rows of ts3_clip_tensor."},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1397,3 +1397,4 @@ ts3_status ts3_layer_forward_noalloc(const ts3_desc *desc, const ts3_weights *w,
 
 #include "ts3_stack.h"
 #include "ts3_train.h"
+#include "ts3_conditioned.h"
