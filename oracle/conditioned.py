@@ -16,10 +16,18 @@ def present(B, S, lengths=None, mask=None):
     return there if mask is None else there & mask
 
 
+def _heads(t, there, G):
+    """[B, S, Hkv, D] as [B, H, S, D] by query head, zero where absent."""
+    return np.repeat(np.where(there[..., None, None], t, 0.0), G, axis=2).transpose(0, 2, 1, 3)
+
+
+def _rows(t):
+    return t.transpose(0, 2, 1, 3)
+
+
 def cross_weights(q, k, there, scale):
     """p [B, H, N, S] and lse [B, H, N]; rows of no state are zero and minus infinity."""
-    G = q.shape[2] // k.shape[2]
-    s = scale * np.einsum("bnhd,bshd->bhns", q, np.repeat(np.where(there[..., None, None], k, 0.0), G, axis=2))
+    s = scale * (_rows(q) @ _heads(k, there, q.shape[2] // k.shape[2]).swapaxes(2, 3))
     s = np.where(there[:, None, None, :], s, -np.inf)
     top = s.max(axis=3, initial=-np.inf, keepdims=True)
     e = np.exp(s - np.where(np.isinf(top), 0.0, top))
@@ -32,8 +40,7 @@ def cross_weights(q, k, there, scale):
 def cross_forward(q, k, v, there, scale):
     """out [B, N, H, D] and lse [B, H, N]."""
     p, lse = cross_weights(q, k, there, scale)
-    v = np.repeat(np.where(there[..., None, None], v, 0.0), q.shape[2] // k.shape[2], axis=2)
-    return np.einsum("bhns,bshd->bnhd", p, v), lse
+    return _rows(p @ _heads(v, there, q.shape[2] // k.shape[2])), lse
 
 
 def cross_backward(q, k, v, there, scale, g):
@@ -41,20 +48,18 @@ def cross_backward(q, k, v, there, scale, g):
     B, S, HK, D = k.shape
     G = q.shape[2] // HK
     p, _ = cross_weights(q, k, there, scale)
-    k, v = (np.repeat(np.where(there[..., None, None], t, 0.0), G, axis=2) for t in (k, v))
+    q, g, k, v = _rows(q), _rows(g), _heads(k, there, G), _heads(v, there, G)
 
     def shared(t):
-        return t.reshape(B, S, HK, G, D).sum(axis=3)
-    out = np.einsum("bhns,bshd->bnhd", p, v)
-    dp = np.einsum("bnhd,bshd->bhns", g, v)
-    ds = p * (dp - np.einsum("bnhd,bnhd->bhn", g, out)[..., None])
-    grads = {"dq": scale * np.einsum("bhns,bshd->bnhd", ds, k), "dk": scale * shared(np.einsum("bhns,bnhd->bshd", ds, q)),
-             "dv": shared(np.einsum("bhns,bnhd->bshd", p, g))}
+        return t.reshape(B, HK, G, S, D).sum(axis=2).transpose(0, 2, 1, 3)
+    out = p @ v
+    ds = p * (g @ v.swapaxes(2, 3) - (g * out).sum(3, keepdims=True))
+    grads = {"dq": scale * _rows(ds @ k), "dk": scale * shared(ds.swapaxes(2, 3) @ q), "dv": shared(p.swapaxes(2, 3) @ g)}
     av, ag = np.abs(v), np.abs(g)
-    terms = p * (np.einsum("bnhd,bshd->bhns", ag, av) + np.einsum("bnhd,bhns,bshd->bhn", ag, p, av, optimize=True)[..., None])
-    sizes = {"out": np.einsum("bhns,bshd->bnhd", p, av), "dq": scale * np.einsum("bhns,bshd->bnhd", terms, np.abs(k)),
-             "dk": scale * shared(np.einsum("bhns,bnhd->bshd", terms, np.abs(q))),
-             "dv": shared(np.einsum("bhns,bnhd->bshd", p, ag))}
+    size = p @ av
+    terms = p * (ag @ av.swapaxes(2, 3) + (ag * size).sum(3, keepdims=True))
+    sizes = {"out": _rows(size), "dq": scale * _rows(terms @ np.abs(k)), "dk": scale * shared(terms.swapaxes(2, 3) @ np.abs(q)),
+             "dv": shared(p.swapaxes(2, 3) @ ag)}
     return grads, sizes
 
 

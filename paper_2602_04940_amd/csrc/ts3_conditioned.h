@@ -10,6 +10,7 @@ struct ts3_cross {
     ts3_cross_desc desc{};
     Workspace part;   // parts of split loops
     Workspace delta;  // the backward's g.out
+    bool lds = false;  // whether the kernels that fill a compute unit's LDS may
     int64_t bytes = 0;
 };
 struct ts3_sandwich {
@@ -73,7 +74,8 @@ ts3_status cross_inputs(const ts3_cross *h, const ts3_cross_inputs &in, CrossArg
     A.mask = in.mask;
     A.B = in.B, A.N = in.N, A.S = in.S, A.H = h->desc.H, A.G = h->desc.H / h->desc.Hkv, A.D = h->desc.D;
     A.scale = h->desc.scale > 0.f ? h->desc.scale : (float)(1.0 / std::sqrt((double)h->desc.D));
-    A.splits = 1;
+    A.by_heads = CrossDiv((uint32_t)h->desc.Hkv);
+    A.by_G = CrossDiv((uint32_t)A.G);
     return TS3_OK;
 }
 // Refuses outputs that overlap an input or one another.
@@ -86,11 +88,32 @@ ts3_status cross_overlaps(std::initializer_list<Range> ins, std::initializer_lis
     }
     return TS3_OK;
 }
-// Splits `tiles` of a loop so that `wgs` workgroups become about `target`, each of two tiles at least.
-void cross_split(CrossArgs &A, int64_t wgs, int64_t tiles, int64_t target) {
+// Splits `tiles` of a loop so that the workgroups (of `blocks` blocks per sample and shared head) become
+// about `target`, each of two tiles at least.
+void cross_split(CrossArgs &A, int64_t blocks, int64_t tiles, int64_t target) {
+    const int64_t wgs = (int64_t)A.B * (A.H / A.G) * blocks;
     const int64_t s = std::max<int64_t>(1, std::min(target / std::max<int64_t>(wgs, 1), tiles / 2));
     A.per = (int32_t)std::max<int64_t>(1, (tiles + s - 1) / s);
     A.splits = (int32_t)std::max<int64_t>(1, (tiles + A.per - 1) / A.per);
+    A.by_splits = CrossDiv((uint32_t)A.splits);
+    A.by_blocks = CrossDiv((uint32_t)std::max<int64_t>(blocks, 1));
+}
+
+template <int P, int DP> ts3_status cross_allow_lds(ts3_cross *h) {
+    if (h->lds) return TS3_OK;
+    HIP_TRY(hipFuncSetAttribute((const void *)&k_cross_fwd_all<P, DP>, hipFuncAttributeMaxDynamicSharedMemorySize, ATTN_LDS_MAX));
+    HIP_TRY(hipFuncSetAttribute((const void *)&k_cross_dq_all<P, DP>, hipFuncAttributeMaxDynamicSharedMemorySize, ATTN_LDS_MAX));
+    h->lds = true;
+    return TS3_OK;
+}
+
+// Workgroups per sample and shared head of the kernels that hold all states in LDS; 0 where these do not
+// fit, or where the rows are too few.
+template <typename All> int64_t cross_all(const CrossArgs &A, int64_t cus) {
+    if (!All::FITS || A.S == 0 || All::bytes(A.S) > All::LDS) return 0;
+    // A wave's blocks of 32 rows: four at least, or filling LDS and uneven ends cost more than it saves.
+    const int64_t blocks = ((int64_t)A.N * A.G + 31) / 32, bh = (int64_t)A.B * (A.H / A.G);
+    return blocks * bh < 4 * All::W * cus ? 0 : std::max<int64_t>(1, cus / bh);
 }
 
 }  // namespace
@@ -153,8 +176,8 @@ ts3_status ts3_cross_forward(ts3_cross *h, const ts3_cross_inputs *in, void *out
         hipStream_t st = (hipStream_t)stream;
         auto launch = [&](auto nq, auto w) -> ts3_status {
             constexpr int NQ = decltype(nq)::value, W = decltype(w)::value, TK = cross_tile<P, DP, W>();
-            const int64_t wgs = bh * ((R + 32 * NQ * W - 1) / (32 * NQ * W));
-            cross_split(A, wgs, (A.S + TK - 1) / TK, (W == 1 ? 8 : 2) * cus);
+            const int64_t blocks = (R + 32 * NQ * W - 1) / (32 * NQ * W), wgs = bh * blocks;
+            cross_split(A, blocks, (A.S + TK - 1) / TK, (W == 1 ? 8 : 2) * cus);
             if (A.splits > 1) {
                 ts3_status r = h->part.reserve(A.splits * bh * R * (DP + 4) * 4, st, h->bytes);
                 if (r != TS3_OK) return r;
@@ -168,9 +191,20 @@ ts3_status ts3_cross_forward(ts3_cross *h, const ts3_cross_inputs *in, void *out
             }
             return TS3_OK;
         };
-        if (R <= 32) return launch(ic<1>{}, ic<1>{});
-        if constexpr (P == 1 && DP <= 64)
-            if (bh * ((R + 255) / 256) >= 2 * cus) return launch(ic<2>{}, ic<4>{});
+        // A wave of its own for a row or a few (float32 heads of 128 would not fit its registers).
+        if constexpr (DP * P <= 192)
+            if (R <= 32) return launch(ic<1>{}, ic<1>{});
+        using All = CrossAll<P, DP, 16>;
+        if constexpr (All::FITS) if (const int64_t per = cross_all<All>(A, cus); per > 0) {
+            if (ts3_status r = cross_allow_lds<P, DP>(h); r != TS3_OK) return r;
+            A.per = (int32_t)per;
+            A.splits = 1;
+            A.by_blocks = CrossDiv((uint32_t)per);
+            const unsigned lds = (unsigned)All::bytes(A.S);
+            hipLaunchKernelGGL((k_cross_fwd_all<P, DP>), dim3((unsigned)(bh * per)), dim3(64 * All::W), lds, st, A);
+            LAUNCH_CHECK("cross attention");
+            return TS3_OK;
+        }
         return launch(ic<1>{}, ic<4>{});
     });
 }
@@ -203,9 +237,17 @@ ts3_status ts3_cross_backward(ts3_cross *h, const ts3_cross_inputs *in, const vo
         const int64_t R = N * A.G, bh = B * HK, cus = device_cu_count();
         hipStream_t st = (hipStream_t)stream;
         CrossArgs Q = A, V = A;
-        const int64_t qwgs = bh * ((R + 127) / 128), vwgs = bh * ((S + 127) / 128);
-        cross_split(Q, qwgs, (S + T - 1) / T, 2 * cus);
-        cross_split(V, vwgs, (R + T - 1) / T, 2 * cus);
+        const int64_t qblocks = (R + 127) / 128, vblocks = (S + 127) / 128, qwgs = bh * qblocks, vwgs = bh * vblocks;
+        cross_split(Q, qblocks, (S + T - 1) / T, 2 * cus);
+        using All = CrossAll<P, DP, 12>;
+        const int64_t qall = cross_all<All>(A, cus);
+        if (qall > 0) {
+            Q.per = (int32_t)qall;
+            Q.splits = 1;
+            Q.by_splits = CrossDiv(1);
+            Q.by_blocks = CrossDiv((uint32_t)qall);
+        }
+        cross_split(V, vblocks, (R + T - 1) / T, (DP * P <= 48 ? 3 : 2) * cus);
         const int64_t qn = bh * R * DP, vn = states * D;
         // one after the other: the parts share their memory
         const int64_t need = std::max(Q.splits > 1 ? Q.splits * qn * 4 : 0, V.splits > 1 ? 2 * V.splits * vn * 4 : 0);
@@ -215,8 +257,15 @@ ts3_status ts3_cross_backward(ts3_cross *h, const ts3_cross_inputs *in, const vo
         Q.part = V.part = (float *)h->part.p;
         V.part2 = V.part + V.splits * vn;
         Q.delta = V.delta = (float *)h->delta.p;
-        if (R > 0) {
-            Q.to = dq;
+        Q.to = dq;
+        if (R > 0 && qall > 0) {
+            if constexpr (All::FITS) {
+                if (ts3_status r = cross_allow_lds<P, DP>(h); r != TS3_OK) return r;
+                hipLaunchKernelGGL((k_cross_dq_all<P, DP>), dim3((unsigned)(bh * qall)), dim3(64 * All::W), (unsigned)All::bytes(S),
+                                   st, Q);
+            }
+            LAUNCH_CHECK("cross attention dq");
+        } else if (R > 0) {
             hipLaunchKernelGGL((k_cross_dq<P, DP>), dim3((unsigned)(qwgs * Q.splits)), dim3(256), 0, st, Q);
             LAUNCH_CHECK("cross attention dq");
             if (Q.splits > 1) {

@@ -32,6 +32,24 @@
 
 namespace ts3 {
 
+// Eight consecutive values of a row.
+__device__ __forceinline__ void load8f(const bf16_t *p, float (&v)[8]) {
+    const u32x4 u = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(u[i] << 16);
+        v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void load8f(const float *p, float (&v)[8]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const f32x4 u = *reinterpret_cast<const f32x4 *>(p + 4 * h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[4 * h + i] = u[i];
+    }
+}
+
 // LDS tile: rows of DP values in 16-byte pieces, piece c of row R at c ^ cross_swz(R).  Reads of 16
 // rows' pieces (ds_read_b128; rows distinct mod 16 in a cycle) and transposing reads of four rows' 64
 // bytes then touch all 64 banks once.
@@ -47,35 +65,53 @@ template <int P, int DP, int ROWS, int THREADS> struct CrossTile {
     using T = typename GatedIO<P>::T;
     static constexpr int NPC = DP / 8, PLANE = ROWS * DP * 2, BYTES = P * PLANE;
     static constexpr int TOTAL = ROWS * NPC, ITEMS = (TOTAL + THREADS - 1) / THREADS;
+    static constexpr int STEP = THREADS / NPC;  // rows from one item of a thread to its next
     u32x4 r[ITEMS][P == 1 ? 1 : 2];
 
-    // at(row): the row's address, always readable.  Columns past D are zero.
+    __device__ __forceinline__ static int row0() { return threadIdx.x / NPC % ROWS; }
+    __device__ __forceinline__ static int col0(int D) {
+        const int c = threadIdx.x % NPC * 8;
+        return c < D ? c : 0;  // columns past D are read from the first and dropped
+    }
+    __device__ __forceinline__ void item(int k, const T *p) {
+#pragma unroll
+        for (int h = 0; h < (P == 1 ? 1 : 2); ++h) r[k][h] = *reinterpret_cast<const u32x4 *>(p + 4 * h);
+    }
+    // Items at equal steps from the thread's first, rows past `end` read from `safe` instead.
+    __device__ __forceinline__ void load(const T *p, int64_t step, int end, const T *safe) {
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) item(k, row0() + k * STEP < end ? p + k * step : safe);
+    }
+    // at(row): the row's address, always readable.
     template <typename F> __device__ __forceinline__ void load(int D, F at) {
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            const int i = threadIdx.x + k * THREADS, row = i / NPC % ROWS, c = i % NPC * 8;
-            const T *const p = at(row) + (c < D ? c : 0);
-#pragma unroll
-            for (int h = 0; h < (P == 1 ? 1 : 2); ++h)
-                r[k][h] = *reinterpret_cast<const u32x4 *>(p + 4 * h);
-        }
+        for (int k = 0; k < ITEMS; ++k) item(k, at((threadIdx.x + k * THREADS) / NPC % ROWS) + col0(D));
     }
-    // there(row): whether the row is there; others are zero, whatever they hold.
-    template <typename F> __device__ __forceinline__ void store(unsigned char *tile, int D, F there) const {
+    // there(row): whether the row is there; others are zero, whatever they hold.  `all`: every row is.
+    template <typename F> __device__ __forceinline__ void store(unsigned char *tile, int D, bool all, F there) const {
+        const bool cin = threadIdx.x % NPC * 8 < D;
 #pragma unroll
         for (int k = 0; k < ITEMS; ++k) {
             const int i = threadIdx.x + k * THREADS, row = i / NPC, pc = i % NPC;
             if (TOTAL % THREADS && i >= TOTAL) continue;
-            const bool in = pc * 8 < D && there(row);
             unsigned char *const to = tile + row * (DP * 2) + ((pc ^ cross_swz<DP>(row)) << 4);
-            if constexpr (P == 1) {
-                *reinterpret_cast<u32x4 *>(to) = in ? r[k][0] : u32x4{0, 0, 0, 0};
-            } else {
-                float v[8];
+            u32x4 v[P == 1 ? 1 : 2];
 #pragma unroll
-                for (int t = 0; t < 8; ++t) v[t] = in ? __uint_as_float(r[k][t >> 2][t & 3]) : 0.f;
+            for (int h = 0; h < (P == 1 ? 1 : 2); ++h) v[h] = r[k][h];
+            if (!(all && D == DP)) {
+                asm volatile("");  // a branch, not selections
+                const bool in = cin && there(row);
+#pragma unroll
+                for (int h = 0; h < (P == 1 ? 1 : 2); ++h) v[h] = in ? v[h] : u32x4{0, 0, 0, 0};
+            }
+            if constexpr (P == 1) {
+                *reinterpret_cast<u32x4 *>(to) = v[0];
+            } else {
+                float x[8];
+#pragma unroll
+                for (int t = 0; t < 8; ++t) x[t] = __uint_as_float(v[t >> 2][t & 3]);
                 Parts<3> f;
-                split8(v, f);
+                split8(x, f);
 #pragma unroll
                 for (int q = 0; q < 3; ++q) *reinterpret_cast<bf16x8 *>(to + q * PLANE) = f.p[q];
             }
@@ -126,6 +162,16 @@ template <int DP> struct CrossColRead {
     }
 };
 
+// Division by a number that the host knows, exact for 32-bit operands: the upper half of the product
+// with floor(2^64 / d) + 1.
+struct CrossDiv {
+    uint32_t d;
+    uint64_t m;
+    __host__ CrossDiv(uint32_t d = 1) : d(d), m(~uint64_t(0) / d + 1) {}
+    // d = 1 gives m = 0 (2^64)
+    __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return m ? (uint32_t)__umul64hi(n, m) : n; }
+};
+
 // Strides in elements: of a sample, a row (point or state) and a head.
 struct CrossView {
     const void *p;
@@ -138,24 +184,25 @@ struct CrossArgs {
     int32_t B, N, S, H, G, D;   // G query heads share a head of keys and values
     float scale;
     int32_t splits, per;        // of a loop: parts, and tiles per part
+    CrossDiv by_splits, by_heads, by_blocks, by_G;
     float *lse, *delta;         // [B][H][N]
     void *to, *to2;             // results (out, dq, or dk and dv), contiguous
     float *part, *part2;        // of split loops
-    __device__ __forceinline__ int heads() const { return H / G; }
+    __device__ __forceinline__ int heads() const { return (int)by_heads.d; }
     __device__ __forceinline__ int rows() const { return N * G; }
 };
 __device__ __forceinline__ float *cross_stat(float *p, const CrossArgs &A, int b, int hk, int r) {
-    const int n = A.G == 1 ? r : r / A.G, h = hk * A.G + (A.G == 1 ? 0 : r % A.G);
+    const int n = A.G == 1 ? r : (int)A.by_G((uint32_t)r), h = hk * A.G + r - n * A.G;
     return p + ((int64_t)b * A.H + h) * A.N + n;
 }
 template <typename T>
 __device__ __forceinline__ const T *cross_row(const CrossView &v, const CrossArgs &A, int b, int hk, int r) {
-    const int n = A.G == 1 ? r : r / A.G, h = hk * A.G + (A.G == 1 ? 0 : r % A.G);
+    const int n = A.G == 1 ? r : (int)A.by_G((uint32_t)r), h = hk * A.G + r - n * A.G;
     return (const T *)v.p + b * v.sb + n * v.sr + h * v.sh;
 }
 // Row r of a contiguous [B][N][H][D] result.
 template <typename T> __device__ __forceinline__ T *cross_to(T *p, const CrossArgs &A, int b, int hk, int r) {
-    const int n = A.G == 1 ? r : r / A.G, h = hk * A.G + (A.G == 1 ? 0 : r % A.G);
+    const int n = A.G == 1 ? r : (int)A.by_G((uint32_t)r), h = hk * A.G + r - n * A.G;
     return p + (((int64_t)b * A.N + n) * A.H + h) * A.D;
 }
 // States of sample b that may be there: those before its length.
@@ -168,14 +215,12 @@ __device__ __forceinline__ int cross_length(const CrossArgs &A, int b) {
 // and then the head, so that consecutive workgroups, which share an L2, read the same lines.
 struct CrossAt {
     int b, hk, blk, split;
-    __device__ __forceinline__ CrossAt(const CrossArgs &A, int blocks) {
-        int i = xcd_remap(blockIdx.x, gridDim.x);
-        split = i % A.splits;
-        i /= A.splits;
-        hk = i % A.heads();
-        i /= A.heads();
-        blk = i % blocks;
-        b = i / blocks;
+    __device__ __forceinline__ explicit CrossAt(const CrossArgs &A) {
+        const uint32_t i = (uint32_t)xcd_remap(blockIdx.x, gridDim.x), j = A.by_splits(i), k = A.by_heads(j), l = A.by_blocks(k);
+        split = (int)(i - j * A.by_splits.d);
+        hk = (int)(j - k * A.by_heads.d);
+        blk = (int)(k - l * A.by_blocks.d);
+        b = (int)l;
     }
 };
 
@@ -197,6 +242,56 @@ __device__ __forceinline__ void cross_load_row(const typename GatedIO<P>::T *row
     }
 }
 
+// The stationary operand of the scores.  Where float32 or narrow heads allow, it is scaled by scale
+// log2(e) beforehand, so that the scores leave the matrix cores as exponents of two, less what their
+// accumulators start from (a maximum, or the logarithm of a sum): no vector instruction per score but
+// the exponential.  A scaled bfloat16 value is carried as two parts (16 bits), whose second product costs
+// what the multiplication would have cost the vector ALU; heads wider than 32 have as much matrix
+// work as vector work, and scale afterwards.
+template <int P, int DP> struct CrossScore {
+    static constexpr bool PRE = P == 3 || DP <= 32;
+    static constexpr int KS = DP / 16, NP = P == 3 ? 3 : PRE ? 2 : 1;
+    Parts<NP> f[KS];
+    __device__ __forceinline__ void load(const typename GatedIO<P>::T *row, int D, bool in, float scale2) {
+        const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int c = 16 * ks + 8 * g;
+            const typename GatedIO<P>::T *const p = row + (c < D ? c : 0);
+            const bool here = in && c < D;
+            if constexpr (PRE) {
+                float v[8];
+                load8f(p, v);
+#pragma unroll
+                for (int t = 0; t < 8; ++t) v[t] *= scale2;
+                if constexpr (P == 3) split8(v, f[ks]);
+                else {
+                    Parts<3> q;
+                    split8(v, q);
+                    f[ks].p[0] = q.p[0];
+                    f[ks].p[1] = q.p[1];
+                }
+            } else {
+                load_parts(p, f[ks]);
+            }
+            if (!(in && D == DP)) {
+                asm volatile("");  // a branch, not selections
+#pragma unroll
+                for (int q = 0; q < NP; ++q) f[ks].p[q] = here ? f[ks].p[q] : bf16x8{};
+            }
+        }
+    }
+    // d += a times step ks, smallest products first
+    __device__ __forceinline__ void mma(f32x16 &d, const Parts<P> &a, int ks) const {
+        if constexpr (P == 3) mma_parts<32, 3>(d, a, f[ks]);
+        else {
+            if constexpr (PRE) Mat<32>::mma(d, a.p[0], f[ks].p[1]);
+            Mat<32>::mma(d, a.p[0], f[ks].p[0]);
+        }
+    }
+};
+__device__ __forceinline__ f32x16 splat16(float v) { return f32x16{v, v, v, v, v, v, v, v, v, v, v, v, v, v, v, v}; }
+
 // Which of the tile's states from `first` are there; bit j is state first + j.
 __device__ __forceinline__ uint64_t cross_present(const CrossArgs &A, unsigned char m, int first, int len, int tile) {
     const int j = threadIdx.x & 63;
@@ -207,183 +302,323 @@ __device__ __forceinline__ unsigned char cross_mask(const CrossArgs &A, int b, i
     return A.mask ? A.mask[(int64_t)b * A.S + (j < len ? j : 0)] : 1;
 }
 
+// The sum of the weights and their operand.  In bfloat16 the sum is of the rounded weights, which then add
+// to one: 0.5 vector instructions a weight instead of one.
+__device__ __forceinline__ float cross_weights(const float (&x)[8], Parts<1> &w, float sum) {
+    to_parts(x, w);
+    return sum_slots(w.p[0], sum);
+}
+__device__ __forceinline__ float cross_weights(const float (&x)[8], Parts<3> &w, float sum) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += x[e];
+    to_parts(x, w);
+    return sum;
+}
+
+// 32 NQ rows of a wave on their way through the states.
+//
+// The exponents are taken against a base per row, which need not be the maximum.  It is zero where the
+// row's first 32 states have a sum of weights of 2^-16 at least then, or else their maximum; afterwards
+// only what lies so far above that a lane's sum of 16 weights reaches 2^40 moves it.  The 32 states are
+// then done over, and the maximum is not looked for otherwise.  In float32 and bfloat16 the weights'
+// precision does not depend on the base.
+template <int P, int DP, int NQ> struct CrossRows {
+    using T = typename GatedIO<P>::T;
+    using Score = CrossScore<P, DP>;
+    static constexpr int KS = DP / 16, DB = (DP + 31) / 32;
+    Score qf[NQ];
+    f32x16 o[NQ][DB], start[NQ];  // start: minus the base, where the scores' accumulators begin
+    float base[NQ], l[NQ];
+    float low[NQ];  // what a sum has to reach: something while a row has no base yet, then nothing
+
+    // Rows r0 + 32 i, those past the last read as the last.
+    __device__ __forceinline__ void begin(const CrossArgs &A, const CrossAt &at, int r0) {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            qf[i].load(cross_row<T>(A.q, A, at.b, at.hk, min(r0 + 32 * i, A.rows() - 1)), A.D, true, A.scale * LOG2E);
+            base[i] = l[i] = 0.f;
+            low[i] = 0x1p-16f;
+            start[i] = f32x16{};
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[i][d] = f32x16{};
+        }
+    }
+    // The states 32 u .. + 31 of a tile of keys and one of values; bit j of `here` is whether j is there.
+    __device__ __forceinline__ void step(const unsigned char *kl, const unsigned char *vl, int plane, int u, uint32_t here,
+                                         const CrossRowRead<DP> &rows, const CrossColRead<DP> &cols, float scale2, int g) {
+        if (here == 0) return;
+        f32x16 s[NQ];
+        // exponents against the base, absent states' at minus infinity
+        auto scores = [&]() {
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) s[i] = Score::PRE ? start[i] : f32x16{};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                Parts<P> a;
+                rows.template read<P>(kl, plane, u, ks, a);
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) qf[i].mma(s[i], a, ks);
+            }
+            if constexpr (!Score::PRE)
+#pragma unroll
+                for (int i = 0; i < NQ; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) s[i][v] = fmaf(s[i][v], scale2, -base[i]);
+            if (here != ~0u) {
+                uint32_t bits = here >> (16 * g);
+                asm("" : "+v"(bits));  // or the bits are taken apart where no state is absent, too
+#pragma unroll
+                for (int i = 0; i < NQ; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) s[i][v] = bits >> v & 1 ? s[i][v] : -INFINITY;
+            }
+        };
+        float sum[NQ];
+        Parts<P> w[NQ][2];
+#pragma unroll 1
+        for (bool again = false;; again = true) {
+            scores();
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                sum[i] = 0.f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = fast_exp2(s[i][8 * h + e]);
+                    sum[i] = cross_weights(x, w[i][h], sum[i]);
+                }
+            }
+            if (again) break;
+            bool high = false;
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) high = high || !(sum[i] < 0x1p40f && sum[i] >= low[i]);
+            if (!__any(high)) {
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) low[i] = 0.f;
+                break;
+            }
+            scores();
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                // a row moves by its own sums alone: the others' results do not depend on it
+                const unsigned out = !(sum[i] < 0x1p40f && sum[i] >= low[i]);
+                const auto sw = __builtin_amdgcn_permlane32_swap(out, out, false, false);
+                const bool moves = sw[0] | sw[1], have = low[i] == 0.f;
+                float mx = -INFINITY;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[i][v]);
+                const auto mw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                mx = fmaxf(__uint_as_float(mw[0]), __uint_as_float(mw[1]));
+                const float up = !moves || mx == -INFINITY ? 0.f : have ? fmaxf(mx, 0.f) : mx;
+                const float alpha = have ? fast_exp2(-up) : 1.f;
+                if (!moves || mx > -INFINITY) low[i] = 0.f;
+                base[i] += up;
+                start[i] = splat16(-base[i]);
+                l[i] *= alpha;
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[i][d] *= alpha;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) l[i] += sum[i];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                Parts<P> a;
+                cols.template read<P>(vl, plane, u, h, d, a);
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) mma_parts<32, P>(o[i][d], a, w[i][h]);
+            }
+    }
+    __device__ __forceinline__ void finish(const CrossArgs &A, const CrossAt &at, int r0, int g) const {
+        const int R = A.rows();
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            const int r = r0 + 32 * i;
+            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[i]), __float_as_uint(l[i]), false, false);
+            const float sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+            if (r >= R) continue;
+            if (A.splits == 1) {
+                // no state: weights of zero, whose sum is minus infinity in the logarithm
+                const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                T *const to = cross_to((T *)A.to, A, at.b, at.hk, r);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const int c = 32 * d + 16 * g;
+                    float x[16];
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) x[v] = o[i][d][v] * inv;
+                    if (c < A.D) store_row<16>(to + c, x);
+                }
+                if (g == 0) *cross_stat(A.lse, A, at.b, at.hk, r) = sum == 0.f ? -INFINITY : (base[i] + log2f(sum)) * LN2;
+            } else {
+                // part[split][b][hk][r][DP + 4]: unscaled sums, their base and their weights' sum
+                const int64_t row = (((int64_t)at.split * A.B + at.b) * A.heads() + at.hk) * R + r;
+                float *const to = A.part + row * (DP + 4);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const int c = 32 * d + 16 * g;
+                    float x[16];
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) x[v] = o[i][d][v];
+                    if (c < A.D) store_row<16>(to + c, x);
+                }
+                if (g == 0) {
+                    to[DP] = sum == 0.f ? -INFINITY : base[i];
+                    to[DP + 1] = sum;
+                }
+            }
+        }
+    }
+};
+
 // Workgroup (b, hk, block, split): 32 NQ rows per wave, W waves, against the split's tiles of
 // states.  The next tile is on its way to registers while this one is used, and goes to the other
-// half of LDS after it.
+// half of LDS after it (a wave alone needs one half: its own reads come first).
 template <int P, int DP, int NQ, int W>
-__global__ __launch_bounds__(64 * W) void k_cross_fwd(const CrossArgs A) {
+__global__ __launch_bounds__(64 * W, W == 4 ? (DP * P <= 32 ? 4 : DP * P <= 96 ? 2 : 1) : 1) void k_cross_fwd(const CrossArgs A) {
     using T = typename GatedIO<P>::T;
-    constexpr int TK = cross_tile<P, DP, W>(), SUB = TK / 32, KS = DP / 16, DB = (DP + 31) / 32;
+    constexpr int TK = cross_tile<P, DP, W>(), SUB = TK / 32, HALVES = W == 1 ? 1 : 2;
     using Tile = CrossTile<P, DP, TK, 64 * W>;
-    __shared__ __align__(16) unsigned char lds[2][2][Tile::BYTES];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, D = A.D, R = A.rows();
-    const CrossAt at(A, (R + 32 * NQ * W - 1) / (32 * NQ * W));
+    __shared__ __align__(16) unsigned char lds[HALVES][2][Tile::BYTES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, D = A.D;
+    const CrossAt at(A);
     const int len = cross_length(A, at.b), tiles = (len + TK - 1) / TK;
     const int t0 = at.split * A.per, t1 = min(tiles, t0 + A.per);
     const int r0 = (at.blk * W + wave) * 32 * NQ + (lane & 31);
     const T *const kb = (const T *)A.k.p + at.b * A.k.sb + at.hk * A.k.sh;
     const T *const vb = (const T *)A.v.p + at.b * A.v.sb + at.hk * A.v.sh;
-    Parts<P> qf[NQ][KS];
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-        const int r = r0 + 32 * i;
-        cross_load_row<P, DP>(cross_row<T>(A.q, A, at.b, at.hk, min(r, R - 1)), D, true, qf[i]);
-    }
-    typename Mat<32>::D o[NQ][DB];
-    float m[NQ], l[NQ];
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-        m[i] = -INFINITY;
-        l[i] = 0.f;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) o[i][d] = typename Mat<32>::D{};
-    }
-    const float scale2 = A.scale * LOG2E;
+    CrossRows<P, DP, NQ> q;
+    q.begin(A, at, r0);
     const CrossRowRead<DP> rows(lane);
     const CrossColRead<DP> cols(lane);
     Tile kt, vt;
+    const T *const kz = kb + Tile::col0(D), *const vz = vb + Tile::col0(D);
+    const T *kp = kz + ((int64_t)Tile::row0() + (int64_t)t0 * TK) * A.k.sr, *vp = vz + ((int64_t)Tile::row0() + (int64_t)t0 * TK) * A.v.sr;
+    const int64_t ks = TK * A.k.sr, vs = TK * A.v.sr;
     auto fetch = [&](int t) {
         const int first = t * TK;
-        kt.load(D, [&](int row) { return kb + (int64_t)min(first + row, len - 1) * A.k.sr; });
-        vt.load(D, [&](int row) { return vb + (int64_t)min(first + row, len - 1) * A.v.sr; });
+        kt.load(kp, Tile::STEP * A.k.sr, len - first, kz);
+        vt.load(vp, Tile::STEP * A.v.sr, len - first, vz);
+        kp += ks;
+        vp += vs;
         return cross_mask(A, at.b, first, len);
     };
+    constexpr uint64_t ALL = TK == 64 ? ~0ull : (1ull << TK) - 1;
+    // absent values are cleared, which weights of zero multiply; absent keys' scores are replaced
     auto put = [&](int t, uint64_t there) {
-        kt.store(lds[t & 1][0], D, [&](int row) { return (there >> row & 1) != 0; });
-        vt.store(lds[t & 1][1], D, [&](int row) { return (there >> row & 1) != 0; });
+        kt.store(lds[t & (HALVES - 1)][0], D, true, [](int) { return true; });
+        vt.store(lds[t & (HALVES - 1)][1], D, there == ALL, [&](int row) { return (there >> row & 1) != 0; });
     };
     uint64_t there = 0;
+    unsigned char mb = 0;
     if (t0 < t1) {
-        const unsigned char mb = fetch(t0);
+        mb = fetch(t0);
         there = cross_present(A, mb, t0 * TK, len, TK);
         put(t0, there);
     }
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
-        unsigned char mb = 0;
         if (t + 1 < t1) mb = fetch(t + 1);
-        const unsigned char *const kl = lds[t & 1][0], *const vl = lds[t & 1][1];
-        if (there) {
-            typename Mat<32>::D s[NQ][SUB];
+        const unsigned char *const kl = lds[t & (HALVES - 1)][0], *const vl = lds[t & (HALVES - 1)][1];
 #pragma unroll
-            for (int i = 0; i < NQ; ++i)
-#pragma unroll
-                for (int u = 0; u < SUB; ++u) s[i][u] = typename Mat<32>::D{};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                for (int u = 0; u < SUB; ++u) {
-                    Parts<P> a;
-                    rows.template read<P>(kl, Tile::PLANE, u, ks, a);
-#pragma unroll
-                    for (int i = 0; i < NQ; ++i) mma_parts<32, P>(s[i][u], a, qf[i][ks]);
-                }
-            const bool whole = there == (TK == 64 ? ~0ull : (1ull << TK) - 1);
-#pragma unroll
-            for (int i = 0; i < NQ; ++i) {
-                float mx = -INFINITY;
-                if (!whole)
-#pragma unroll
-                    for (int u = 0; u < SUB; ++u) {
-                        const uint32_t bits = (uint32_t)(there >> (32 * u)) >> (16 * g);
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) s[i][u][v] = bits >> v & 1 ? s[i][u][v] : -INFINITY;
-                    }
-#pragma unroll
-                for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[i][u][v]);
-                const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-                mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale2;
-                const float mn = fmaxf(m[i], mx), base = mn == -INFINITY ? 0.f : mn;
-                const float alpha = fast_exp2(m[i] - base);
-                m[i] = mn;
-                float sum = 0.f;
-#pragma unroll
-                for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        s[i][u][v] = fast_exp2(fmaf(s[i][u][v], scale2, -base));
-                        sum += s[i][u][v];
-                    }
-                l[i] = l[i] * alpha + sum;
-                if (__any(alpha != 1.f))
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) o[i][d] *= alpha;
-            }
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    Parts<P> w[NQ];
-#pragma unroll
-                    for (int i = 0; i < NQ; ++i) {
-                        float x[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = s[i][u][8 * h + e];
-                        to_parts(x, w[i]);
-                    }
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) {
-                        Parts<P> a;
-                        cols.template read<P>(vl, Tile::PLANE, u, h, d, a);
-#pragma unroll
-                        for (int i = 0; i < NQ; ++i) mma_parts<32, P>(o[i][d], a, w[i]);
-                    }
-                }
-        }
+        for (int u = 0; u < SUB; ++u)
+            q.step(kl, vl, Tile::PLANE, u, u ? (uint32_t)(there >> 32) : (uint32_t)there, rows, cols, A.scale * LOG2E, g);
+        if constexpr (HALVES == 1) __syncthreads();
         if (t + 1 < t1) {
             there = cross_present(A, mb, (t + 1) * TK, len, TK);
             put(t + 1, there);
         }
         __syncthreads();
     }
+    q.finish(A, at, r0, g);
+}
+
+// The same for many rows and few states: a sample's and head's states all lie in LDS, and the
+// workgroup's W waves go through blocks of 32 rows, with neither loads of states nor barriers between
+// them.  Of the blocks, A.per workgroups (at.blk) take every one in turn, and a workgroup's waves the next
+// one each: dealt out beforehand, the waves of a SIMD, which do not run equally fast, would end
+// apart (a quarter of the waves' time idle in the forward).
+template <int P, int DP, int WAVES> struct CrossAll {
+    static constexpr int TK = cross_tile<P, DP, WAVES>(), W = WAVES;
+    using Tile = CrossTile<P, DP, TK, 64 * W>;
+    static constexpr int TILE = 2 * Tile::BYTES, BATCH = 2;
+    static constexpr int LDS = 160 * 1024;      // a workgroup per compute unit
+    static constexpr bool FITS = DP * P <= 64;  // within the registers of so many waves
+    static constexpr int64_t bytes(int64_t S) { return (S + TK - 1) / TK * (TILE + 8) + 8; }
+    // The first row of the wave's next block.
+    __device__ static __forceinline__ int64_t next(const CrossArgs &A, const CrossAt &at, int *taken) {
+        int i = 0;
+        if ((threadIdx.x & 63) == 0) i = atomicAdd(taken, 1);
+        return ((int64_t)__builtin_amdgcn_readfirstlane(i) * A.per + at.blk) * 32;
+    }
+    // Keys, values (absent ones cleared) and presence of the tiles.
+    __device__ static __forceinline__ void fill(const CrossArgs &A, const CrossAt &at, int len, unsigned char *tiles, uint64_t *present) {
+        using T = typename GatedIO<P>::T;
+        const int n = (len + TK - 1) / TK, D = A.D;
+        const T *const kb = (const T *)A.k.p + at.b * A.k.sb + at.hk * A.k.sh;
+        const T *const vb = (const T *)A.v.p + at.b * A.v.sb + at.hk * A.v.sh;
+        for (int t = 0; t < n; t += BATCH) {
+            Tile kt[BATCH], vt[BATCH];
+            unsigned char m[BATCH];
 #pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-        const int r = r0 + 32 * i;
-        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[i]), __float_as_uint(l[i]), false, false);
-        const float sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-        if (r >= R) continue;
-        if (A.splits == 1) {
-            // no state: weights of zero, whose sum is minus infinity in the logarithm
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            T *const to = cross_to((T *)A.to, A, at.b, at.hk, r);
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                const int c = 32 * d + 16 * g;
-                float x[16];
-#pragma unroll
-                for (int v = 0; v < 16; ++v) x[v] = o[i][d][v] * inv;
-                if (c < D) store_row<16>(to + c, x);
+            for (int i = 0; i < BATCH; ++i) {
+                const int first = (t + i) * TK;
+                kt[i].load(D, [&](int row) { return kb + (int64_t)min(first + row, len - 1) * A.k.sr; });
+                vt[i].load(D, [&](int row) { return vb + (int64_t)min(first + row, len - 1) * A.v.sr; });
+                m[i] = cross_mask(A, at.b, first, len);
             }
-            if (g == 0) *cross_stat(A.lse, A, at.b, at.hk, r) = sum == 0.f ? -INFINITY : (m[i] + log2f(sum)) * LN2;
-        } else {
-            // part[split][b][hk][r][DP + 2]: unscaled sums, their maximum and their weights' sum
-            const int64_t row = (((int64_t)at.split * A.B + at.b) * A.heads() + at.hk) * R + r;
-            float *const to = A.part + row * (DP + 4);
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                const int c = 32 * d + 16 * g;
-                float x[16];
-#pragma unroll
-                for (int v = 0; v < 16; ++v) x[v] = o[i][d][v];
-                if (c < D) store_row<16>(to + c, x);
-            }
-            if (g == 0) {
-                to[DP] = m[i];
-                to[DP + 1] = sum;
+            for (int i = 0; i < BATCH; ++i) {
+                if (t + i >= n) break;
+                const uint64_t there = cross_present(A, m[i], (t + i) * TK, len, TK);
+                auto in = [&](int row) { return (there >> row & 1) != 0; };
+                kt[i].store(tiles + (t + i) * TILE, D, false, in);
+                vt[i].store(tiles + (t + i) * TILE + Tile::BYTES, D, false, in);
+                if (threadIdx.x == 0) present[t + i] = there;
             }
         }
+        __syncthreads();
+    }
+};
+template <int P, int DP>
+__global__ __launch_bounds__(1024, 4) void k_cross_fwd_all(const CrossArgs A) {
+    using All = CrossAll<P, DP, 16>;
+    extern __shared__ __align__(16) unsigned char all_lds[];
+    const CrossAt at(A);
+    const int lane = threadIdx.x & 63, g = lane >> 5, R = A.rows();
+    const int len = cross_length(A, at.b), n = (len + All::TK - 1) / All::TK;
+    uint64_t *const present = (uint64_t *)(all_lds + (size_t)((A.S + All::TK - 1) / All::TK) * All::TILE);
+    int *const taken = (int *)(present + (A.S + All::TK - 1) / All::TK);
+    if (threadIdx.x == 0) *taken = 0;
+    All::fill(A, at, len, all_lds, present);
+    const CrossRowRead<DP> rows(lane);
+    const CrossColRead<DP> cols(lane);
+    for (int64_t first; (first = All::next(A, at, taken)) < R;) {
+        const int r0 = (int)first;
+        CrossRows<P, DP, 1> q;
+        q.begin(A, at, r0 + (lane & 31));
+        for (int t = 0; t < n; ++t) {
+            const uint64_t there = present[t];
+            const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)there), hi = __builtin_amdgcn_readfirstlane((uint32_t)(there >> 32));
+            const unsigned char *const kl = all_lds + t * All::TILE;
+            q.step(kl, kl + All::Tile::BYTES, All::Tile::PLANE, 0, lo, rows, cols, A.scale * LOG2E, g);
+            if constexpr (All::TK == 64) q.step(kl, kl + All::Tile::BYTES, All::Tile::PLANE, 1, hi, rows, cols, A.scale * LOG2E, g);
+        }
+        q.finish(A, at, r0 + (lane & 31), g);
     }
 }
 
-// A row per workgroup: the splits' parts scaled to the largest maximum and added, 256 / DP at a
-// time, then these in order.
+// A row per workgroup: the splits' parts scaled to the largest base and added, 1024 / DP splits at a
+// time by as many groups of lanes, then the groups' sums in order.
 template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_join(const CrossArgs A) {
     using T = typename GatedIO<P>::T;
-    constexpr int NG = 256 / DP;
-    __shared__ float acc[NG][DP], sums[NG], tops[4];
-    const int R = A.rows(), tid = threadIdx.x, c = tid % DP, q = tid / DP;
+    constexpr int LG = DP / 4, NG = 256 / LG;
+    __shared__ __align__(16) float acc[NG][DP];
+    __shared__ float sums[NG], tops[4];
+    const int R = A.rows(), tid = threadIdx.x, c = 4 * (tid % LG), q = tid / LG;
     const int64_t bhr = blockIdx.x, step = (int64_t)A.B * A.heads() * R * (DP + 4);
     const int r = (int)(bhr % R), hk = (int)(bhr / R % A.heads()), b = (int)(bhr / R / A.heads());
     const float *const part = A.part + bhr * (DP + 4);
@@ -395,181 +630,265 @@ template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_join(con
     __syncthreads();
     top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     const float base = top == -INFINITY ? 0.f : top;
-    float v = 0.f, sum = 0.f;
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
     const bool in = c < A.D;
-#pragma unroll 4
+#pragma unroll 8
     for (int s = q; s < A.splits; s += NG) {
         const float *const p = part + s * step;
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(p + (in ? c : 0));
         const float w = fast_exp2(p[DP] - base);
-        v += w * (in ? p[c] : 0.f);
+        v += w * x;
         sum += w * p[DP + 1];
     }
-    acc[q][c] = v;
+    *reinterpret_cast<f32x4 *>(&acc[q][c]) = v;
     if (c == 0) sums[q] = sum;
     __syncthreads();
-    if (q) return;
+    if (tid >= DP) return;
     sum = 0.f;
-    v = 0.f;
+    float y = 0.f;
     for (int i = 0; i < NG; ++i) {
         sum += sums[i];
-        v += acc[i][c];
+        y += acc[i][tid];
     }
-    if (in) cross_to((T *)A.to, A, b, hk, r)[c] = from_float<T>(sum == 0.f ? 0.f : v / sum);
-    if (c == 0) *cross_stat(A.lse, A, b, hk, r) = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
+    if (tid < A.D) cross_to((T *)A.to, A, b, hk, r)[tid] = from_float<T>(sum == 0.f ? 0.f : y / sum);
+    if (tid == 0) *cross_stat(A.lse, A, b, hk, r) = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
 }
 
-// delta = g.out of the rows, and their dq: as the forward's loop, with the values as a second
+// 32 rows of a wave: delta = g.out, and dq from the states they go through, the values being a second
 // operand of rows and the keys read transposed.
-template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_dq(const CrossArgs A) {
+template <int P, int DP> struct CrossSlopes {
     using T = typename GatedIO<P>::T;
-    constexpr int TK = P == 1 && DP < 128 ? 64 : 32, SUB = TK / 32, KS = DP / 16, DB = (DP + 31) / 32;
+    using Score = CrossScore<P, DP>;
+    static constexpr int KS = DP / 16, DB = (DP + 31) / 32;
+    Score qf;
+    Parts<P> gf[KS];
+    f32x16 o[DB], start, dstart;  // minus the logarithm of the sum, and minus delta
+    __device__ __forceinline__ void begin(const CrossArgs &A, const CrossAt &at, int r, int g) {
+        const int rc = min(r, A.rows() - 1), D = A.D;
+        const T *const grow = cross_row<T>(A.g, A, at.b, at.hk, rc), *const orow = cross_row<T>(A.out, A, at.b, at.hk, rc);
+        qf.load(cross_row<T>(A.q, A, at.b, at.hk, rc), D, true, A.scale * LOG2E);
+        cross_load_row<P, DP>(grow, D, true, gf);
+        float delta = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int c = 16 * ks + 8 * g;
+            float x[8], y[8], d = 0.f;
+            load8f(grow + (c < D ? c : 0), x);
+            load8f(orow + (c < D ? c : 0), y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d += x[e] * y[e];
+            delta += c < D ? d : 0.f;
+        }
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(delta), __float_as_uint(delta), false, false);
+        delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+        if (r < A.rows() && g == 0 && at.split == 0) *cross_stat(A.delta, A, at.b, at.hk, r) = delta;
+        start = splat16(-LOG2E * *cross_stat(A.lse, A, at.b, at.hk, rc));
+        dstart = splat16(-delta);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) o[d] = f32x16{};
+    }
+    __device__ __forceinline__ void step(const unsigned char *kl, const unsigned char *vl, int plane, int u, uint32_t here,
+                                         const CrossRowRead<DP> &rows, const CrossColRead<DP> &cols, float scale2, int g) {
+        if (here == 0) return;
+        f32x16 s = Score::PRE ? start : f32x16{}, dp = dstart;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            Parts<P> a;
+            rows.template read<P>(kl, plane, u, ks, a);
+            qf.mma(s, a, ks);
+            rows.template read<P>(vl, plane, u, ks, a);
+            mma_parts<32, P>(dp, a, gf[ks]);
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[v] = fast_exp2(Score::PRE ? s[v] : fmaf(s[v], scale2, start[0])) * dp[v];
+        if (here != ~0u) {
+            uint32_t bits = here >> (16 * g);
+            asm("" : "+v"(bits));
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[v] = bits >> v & 1 ? s[v] : 0.f;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = s[8 * h + e];
+            Parts<P> w;
+            to_parts(x, w);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                Parts<P> a;
+                cols.template read<P>(kl, plane, u, h, d, a);
+                mma_parts<32, P>(o[d], a, w);
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(const CrossArgs &A, const CrossAt &at, int r, int g) const {
+        const int R = A.rows();
+        if (r >= R) return;
+        float *const part = A.part + ((((int64_t)at.split * A.B + at.b) * A.heads() + at.hk) * R + r) * DP;
+        T *const to = cross_to((T *)A.to, A, at.b, at.hk, r);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            const int c = 32 * d + 16 * g;
+            float x[16];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) x[v] = o[d][v] * A.scale;
+            if (c < A.D) {
+                if (A.splits == 1) store_row<16>(to + c, x);
+                else store_row<16>(part + c, x);
+            }
+        }
+    }
+};
+
+// As k_cross_fwd, and as k_cross_fwd_all.
+template <int P, int DP> __global__ __launch_bounds__(256, DP * P <= 96 ? 2 : 1) void k_cross_dq(const CrossArgs A) {
+    using T = typename GatedIO<P>::T;
+    constexpr int TK = P == 1 && DP < 128 ? 64 : 32, SUB = TK / 32;
     using Tile = CrossTile<P, DP, TK, 256>;
     __shared__ __align__(16) unsigned char lds[2][2][Tile::BYTES];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, D = A.D, R = A.rows();
-    const CrossAt at(A, (R + 127) / 128);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, D = A.D;
+    const CrossAt at(A);
     const int len = cross_length(A, at.b), tiles = (len + TK - 1) / TK;
     const int t0 = at.split * A.per, t1 = min(tiles, t0 + A.per);
-    const int r = at.blk * 128 + wave * 32 + (lane & 31), rc = min(r, R - 1);
+    const int r = at.blk * 128 + wave * 32 + (lane & 31);
     const T *const kb = (const T *)A.k.p + at.b * A.k.sb + at.hk * A.k.sh;
     const T *const vb = (const T *)A.v.p + at.b * A.v.sb + at.hk * A.v.sh;
-    Parts<P> qf[KS], gf[KS];
-    const T *const grow = cross_row<T>(A.g, A, at.b, at.hk, rc), *const orow = cross_row<T>(A.out, A, at.b, at.hk, rc);
-    cross_load_row<P, DP>(cross_row<T>(A.q, A, at.b, at.hk, rc), D, true, qf);
-    cross_load_row<P, DP>(grow, D, true, gf);
-    float delta = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-        const int c = 16 * ks + 8 * g;
-        if (c < D)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) delta += to_float(grow[c + e]) * to_float(orow[c + e]);
-    }
-    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(delta), __float_as_uint(delta), false, false);
-    delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    if (r < R && g == 0 && at.split == 0) *cross_stat(A.delta, A, at.b, at.hk, r) = delta;
-    const float scale2 = A.scale * LOG2E, lse2 = *cross_stat(A.lse, A, at.b, at.hk, rc) * LOG2E;
-    typename Mat<32>::D o[DB];
-#pragma unroll
-    for (int d = 0; d < DB; ++d) o[d] = typename Mat<32>::D{};
+    CrossSlopes<P, DP> q;
+    q.begin(A, at, r, g);
     const CrossRowRead<DP> rows(lane);
     const CrossColRead<DP> cols(lane);
     Tile kt, vt;
+    const T *const kz = kb + Tile::col0(D), *const vz = vb + Tile::col0(D);
+    const T *kp = kz + ((int64_t)Tile::row0() + (int64_t)t0 * TK) * A.k.sr, *vp = vz + ((int64_t)Tile::row0() + (int64_t)t0 * TK) * A.v.sr;
+    const int64_t ks = TK * A.k.sr, vs = TK * A.v.sr;
     auto fetch = [&](int t) {
         const int first = t * TK;
-        kt.load(D, [&](int row) { return kb + (int64_t)min(first + row, len - 1) * A.k.sr; });
-        vt.load(D, [&](int row) { return vb + (int64_t)min(first + row, len - 1) * A.v.sr; });
+        kt.load(kp, Tile::STEP * A.k.sr, len - first, kz);
+        vt.load(vp, Tile::STEP * A.v.sr, len - first, vz);
+        kp += ks;
+        vp += vs;
         return cross_mask(A, at.b, first, len);
     };
+    constexpr uint64_t ALL = TK == 64 ? ~0ull : (1ull << TK) - 1;
+    // absent keys are cleared, which slopes of zero multiply; absent values' slopes are replaced
     auto put = [&](int t, uint64_t there) {
-        kt.store(lds[t & 1][0], D, [&](int row) { return (there >> row & 1) != 0; });
-        vt.store(lds[t & 1][1], D, [&](int row) { return (there >> row & 1) != 0; });
+        kt.store(lds[t & 1][0], D, there == ALL, [&](int row) { return (there >> row & 1) != 0; });
+        vt.store(lds[t & 1][1], D, true, [](int) { return true; });
     };
     uint64_t there = 0;
+    unsigned char mb = 0;
     if (t0 < t1) {
-        const unsigned char mb = fetch(t0);
+        mb = fetch(t0);
         there = cross_present(A, mb, t0 * TK, len, TK);
         put(t0, there);
     }
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
-        unsigned char mb = 0;
         if (t + 1 < t1) mb = fetch(t + 1);
         const unsigned char *const kl = lds[t & 1][0], *const vl = lds[t & 1][1];
-        if (there)
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                typename Mat<32>::D s{}, dp{};
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    Parts<P> a;
-                    rows.template read<P>(kl, Tile::PLANE, u, ks, a);
-                    mma_parts<32, P>(s, a, qf[ks]);
-                    rows.template read<P>(vl, Tile::PLANE, u, ks, a);
-                    mma_parts<32, P>(dp, a, gf[ks]);
-                }
-                const uint32_t bits = (uint32_t)(there >> (32 * u)) >> (16 * g);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float p = fast_exp2(fmaf(s[8 * h + e], scale2, -lse2));
-                        x[e] = bits >> (8 * h + e) & 1 ? p * (dp[8 * h + e] - delta) : 0.f;
-                    }
-                    Parts<P> w;
-                    to_parts(x, w);
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) {
-                        Parts<P> a;
-                        cols.template read<P>(kl, Tile::PLANE, u, h, d, a);
-                        mma_parts<32, P>(o[d], a, w);
-                    }
-                }
-            }
+        for (int u = 0; u < SUB; ++u)
+            q.step(kl, vl, Tile::PLANE, u, u ? (uint32_t)(there >> 32) : (uint32_t)there, rows, cols, A.scale * LOG2E, g);
         if (t + 1 < t1) {
             there = cross_present(A, mb, (t + 1) * TK, len, TK);
             put(t + 1, there);
         }
         __syncthreads();
     }
-    if (r >= R) return;
-    float *const part = A.part + ((((int64_t)at.split * A.B + at.b) * A.heads() + at.hk) * R + r) * DP;
-    T *const to = cross_to((T *)A.to, A, at.b, at.hk, r);
-#pragma unroll
-    for (int d = 0; d < DB; ++d) {
-        const int c = 32 * d + 16 * g;
-        float x[16];
-#pragma unroll
-        for (int v = 0; v < 16; ++v) x[v] = o[d][v] * A.scale;
-        if (c < D) {
-            if (A.splits == 1) store_row<16>(to + c, x);
-            else store_row<16>(part + c, x);
+    q.finish(A, at, r, g);
+}
+template <int P, int DP>
+__global__ __launch_bounds__(768, 3) void k_cross_dq_all(const CrossArgs A) {
+    using All = CrossAll<P, DP, 12>;
+    extern __shared__ __align__(16) unsigned char all_lds[];
+    const CrossAt at(A);
+    const int lane = threadIdx.x & 63, g = lane >> 5, R = A.rows();
+    const int len = cross_length(A, at.b), n = (len + All::TK - 1) / All::TK;
+    uint64_t *const present = (uint64_t *)(all_lds + (size_t)((A.S + All::TK - 1) / All::TK) * All::TILE);
+    int *const taken = (int *)(present + (A.S + All::TK - 1) / All::TK);
+    if (threadIdx.x == 0) *taken = 0;
+    All::fill(A, at, len, all_lds, present);
+    const CrossRowRead<DP> rows(lane);
+    const CrossColRead<DP> cols(lane);
+    for (int64_t first; (first = All::next(A, at, taken)) < R;) {
+        const int r0 = (int)first;
+        CrossSlopes<P, DP> q;
+        q.begin(A, at, r0 + (lane & 31), g);
+        for (int t = 0; t < n; ++t) {
+            const uint64_t there = present[t];
+            const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)there), hi = __builtin_amdgcn_readfirstlane((uint32_t)(there >> 32));
+            const unsigned char *const kl = all_lds + t * All::TILE;
+            q.step(kl, kl + All::Tile::BYTES, All::Tile::PLANE, 0, lo, rows, cols, A.scale * LOG2E, g);
+            if constexpr (All::TK == 64) q.step(kl, kl + All::Tile::BYTES, All::Tile::PLANE, 1, hi, rows, cols, A.scale * LOG2E, g);
         }
+        q.finish(A, at, r0 + (lane & 31), g);
     }
 }
 
 // dk and dv of 32 states per wave, four waves, summed over the split's tiles of rows (queries and
 // their output gradients in LDS with the rows' lse and delta).
-template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_dkv(const CrossArgs A) {
+template <int P, int DP> __global__ __launch_bounds__(256, DP * P <= 64 ? 2 : 1) void k_cross_dkv(const CrossArgs A) {
     using T = typename GatedIO<P>::T;
+    using Score = CrossScore<P, DP>;
     constexpr int TR = P == 1 && DP < 128 ? 64 : 32, SUB = TR / 32, KS = DP / 16, DB = (DP + 31) / 32;
     using Tile = CrossTile<P, DP, TR, 256>;
     __shared__ __align__(16) unsigned char lds[2][2][Tile::BYTES];
     __shared__ __align__(16) float stat[2][2][TR];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5, D = A.D, R = A.rows();
-    const CrossAt at(A, (A.S + 127) / 128);
+    const CrossAt at(A);
     const int len = cross_length(A, at.b), tiles = (R + TR - 1) / TR;
     const int j = at.blk * 128 + wave * 32 + (lane & 31), jc = min(j, A.S - 1);
     const bool there = j < len && (!A.mask || A.mask[(int64_t)at.b * A.S + jc]);
     // a block of absent states has nothing to sum
     const int t0 = at.split * A.per, t1 = at.blk * 128 < len ? min(tiles, t0 + A.per) : t0;
-    Parts<P> kf[KS], vf[KS];
-    cross_load_row<P, DP>((const T *)A.k.p + at.b * A.k.sb + jc * A.k.sr + at.hk * A.k.sh, D, there, kf);
+    const float scale2 = A.scale * LOG2E;
+    Score kf;
+    Parts<P> vf[KS];
+    kf.load((const T *)A.k.p + at.b * A.k.sb + jc * A.k.sr + at.hk * A.k.sh, D, there, scale2);
     cross_load_row<P, DP>((const T *)A.v.p + at.b * A.v.sb + jc * A.v.sr + at.hk * A.v.sh, D, there, vf);
     typename Mat<32>::D dk[DB], dv[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) dk[d] = dv[d] = typename Mat<32>::D{};
-    const float scale2 = A.scale * LOG2E;
     const CrossRowRead<DP> rows(lane);
     const CrossColRead<DP> cols(lane);
     Tile qt, gt;
     float st = 0.f;
+    // Where G divides 16, a thread's rows keep their head from item to item and tile to tile.
+    const bool even = 16 % A.G == 0;
+    const int64_t pts = even ? TR / A.G : 0, ptk = even ? Tile::STEP / A.G : 0;  // points a tile, and an item
+    const T *const qz = cross_row<T>(A.q, A, at.b, at.hk, 0) + Tile::col0(D), *const gz = cross_row<T>(A.g, A, at.b, at.hk, 0) + Tile::col0(D);
+    const T *qp = cross_row<T>(A.q, A, at.b, at.hk, Tile::row0() + t0 * TR) + Tile::col0(D);
+    const T *gp = cross_row<T>(A.g, A, at.b, at.hk, Tile::row0() + t0 * TR) + Tile::col0(D);
+    float *const stats = threadIdx.x < TR ? A.lse : A.delta, *const sz = cross_stat(stats, A, at.b, at.hk, 0);
+    const float *sp = cross_stat(stats, A, at.b, at.hk, (int)threadIdx.x % TR + t0 * TR);
     auto fetch = [&](int t) {
         const int first = t * TR;
-        qt.load(D, [&](int row) { return cross_row<T>(A.q, A, at.b, at.hk, min(first + row, R - 1)); });
-        gt.load(D, [&](int row) { return cross_row<T>(A.g, A, at.b, at.hk, min(first + row, R - 1)); });
-        if (threadIdx.x < 2 * TR) {
-            const int row = first + threadIdx.x % TR;
-            // past the last row the weights are e^-inf
-            if (threadIdx.x < TR) st = row < R ? *cross_stat(A.lse, A, at.b, at.hk, row) * LOG2E : INFINITY;
-            else st = row < R ? *cross_stat(A.delta, A, at.b, at.hk, row) : 0.f;
+        if (even) {
+            qt.load(qp, ptk * A.q.sr, R - first, qz);
+            gt.load(gp, ptk * A.g.sr, R - first, gz);
+            if (threadIdx.x < 2 * TR) st = *(first + (int)threadIdx.x % TR < R ? sp : sz);
+            qp += pts * A.q.sr;
+            gp += pts * A.g.sr;
+            sp += pts;
+        } else {
+            qt.load(D, [&](int row) { return cross_row<T>(A.q, A, at.b, at.hk, min(first + row, R - 1)); });
+            gt.load(D, [&](int row) { return cross_row<T>(A.g, A, at.b, at.hk, min(first + row, R - 1)); });
+            if (threadIdx.x < 2 * TR) st = *cross_stat(stats, A, at.b, at.hk, min(first + (int)threadIdx.x % TR, R - 1));
         }
     };
     auto put = [&](int t) {
         const int first = t * TR;
-        qt.store(lds[t & 1][0], D, [&](int row) { return first + row < R; });
-        gt.store(lds[t & 1][1], D, [&](int row) { return first + row < R; });
-        if (threadIdx.x < 2 * TR) stat[t & 1][threadIdx.x / TR][threadIdx.x % TR] = st;
+        const bool all = first + TR <= R;
+        qt.store(lds[t & 1][0], D, all, [&](int row) { return first + row < R; });
+        gt.store(lds[t & 1][1], D, all, [&](int row) { return first + row < R; });
+        if (threadIdx.x < 2 * TR) {
+            // negated, as the accumulators start; past the last row the weights are e^-inf
+            const int row = threadIdx.x % TR;
+            const bool lse = threadIdx.x < TR, in = first + row < R;
+            stat[t & 1][lse ? 0 : 1][row] = lse ? in ? -LOG2E * st : -INFINITY : in ? -st : 0.f;
+        }
     };
     if (t0 < t1) {
         fetch(t0);
@@ -581,29 +900,40 @@ template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_dkv(cons
         const unsigned char *const ql = lds[t & 1][0], *const gl = lds[t & 1][1];
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
-            typename Mat<32>::D s{}, dp{};
+            // what an absent state's column holds stays in it, and is dropped at the end
+            f32x16 s, dp, ls;
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const int row = 32 * u + 16 * g + e;
+                const f32x4 x = *reinterpret_cast<const f32x4 *>(&stat[t & 1][0][row]);
+                const f32x4 y = *reinterpret_cast<const f32x4 *>(&stat[t & 1][1][row]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    ls[e + i] = x[i];
+                    dp[e + i] = y[i];
+                }
+            }
+            s = Score::PRE ? ls : f32x16{};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 Parts<P> a;
                 rows.template read<P>(ql, Tile::PLANE, u, ks, a);
-                mma_parts<32, P>(s, a, kf[ks]);
+                kf.mma(s, a, ks);
                 rows.template read<P>(gl, Tile::PLANE, u, ks, a);
                 mma_parts<32, P>(dp, a, vf[ks]);
+            }
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                s[v] = fast_exp2(Score::PRE ? s[v] : fmaf(s[v], scale2, ls[v]));
+                dp[v] *= s[v];
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 float x[8], y[8];
 #pragma unroll
-                for (int e = 0; e < 8; e += 4) {
-                    const int row = 32 * u + 16 * g + 8 * h + e;
-                    const f32x4 ls = *reinterpret_cast<const f32x4 *>(&stat[t & 1][0][row]);
-                    const f32x4 de = *reinterpret_cast<const f32x4 *>(&stat[t & 1][1][row]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float p = there ? fast_exp2(fmaf(s[8 * h + e + i], scale2, -ls[i])) : 0.f;
-                        x[e + i] = p;
-                        y[e + i] = p * (dp[8 * h + e + i] - de[i]);
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = s[8 * h + e];
+                    y[e] = dp[8 * h + e];
                 }
                 Parts<P> w, z;
                 to_parts(x, w);

@@ -8,9 +8,12 @@ Attention.  A score is a sum of D products of operands carried to u: it is off b
 X = scale |q| |k| at its largest, and so is its weight, relative to itself.  Sums over S states and N
 points walk their square roots.  In float32 every output is then within four times
 (8 + sqrt S + sqrt N + (4 + sqrt D) X) u of the size of its terms (the sum of their absolute values).
-In bfloat16 the output is rounded once (2^-8 of itself), and so are its weights (2^-8 of the size of its
-terms); dq and dk take slopes that are rounded (the same) and g.out from the rounded output (the same
-again: the reference's sizes hold both), where the output's own weights were rounded before (once more).
+In bfloat16 the output is rounded once (2^-8 of itself), and so are its weights p.  Their sum is of the
+rounded ones: with p (1 + e), |e| <= 2^-8, the output is off by sum p e (v - out) / sum p (1 + e), at most 2^-8 of
+the size of its terms and 2^-8 of itself again, and lse by log(1 + 2^-8).  The backward's p are off by as much
+before they are rounded: dv is within 2^-8 of itself and twice 2^-8 of its size.  dq and dk take slopes that
+are rounded (2^-8 of their size), of such p (again), and g.out from the rounded output (again: the
+reference's sizes hold both g.v and g.out), whose own weights were rounded (again).
 
 Norms.  As the other training operators': four walks over C, and over N for sums over rows, of the
 largest value in float32; in bfloat16 2^-8 in the mean square.
@@ -54,10 +57,10 @@ def _check(name, got, ref, size, dtype, walk):
     if ref.size == 0:
         return
     assert np.isfinite(got).all(), name
-    err, rounds = np.abs(got - ref), {"out": 1, "dv": 1, "dq": 3, "dk": 3}[name]
+    err, (own, rounds) = np.abs(got - ref), {"out": (2, 1), "dv": (1, 2), "dq": (1, 4), "dk": (1, 4)}[name]
     bar = 4 * walk * U * size.max()
     if dtype == "bf16":
-        bar = bar + 2.0 ** -8 * (np.abs(ref) + rounds * 1.02 * size)
+        bar = bar + 2.0 ** -8 * (own * np.abs(ref) + rounds * 1.02 * size)
     else:
         bar = np.full_like(err, bar)
     print(f"{name}: normwise {normwise(got, ref):.2e}, of the bar {float((err / np.maximum(bar, 1e-300)).max()):.3f}", flush=True)
@@ -90,7 +93,7 @@ def _compare(q, k, v, g, dtype, there, scale, out, lse, grads):
     empty = np.isinf(ref_lse)
     got = to_host(lse)
     assert (got[empty] == -np.inf).all()
-    assert np.abs(got[~empty] - ref_lse[~empty]).max(initial=0.0) <= 4 * walk * U * (1 + X)
+    assert np.abs(got[~empty] - ref_lse[~empty]).max(initial=0.0) <= 4 * walk * U * (1 + X) + (2.0 ** -8 if dtype == "bf16" else 0)
     for name in ("dq", "dk", "dv"):
         _check(name, grads[name], refs[name], sizes[name], dtype, walk)
         if name != "dq":
@@ -105,7 +108,7 @@ CROSS = [(1, 1, 1, 1, 1, 16), (1, 1, 700, 8, 8, 32), (2, 1, 3001, 8, 2, 64), (3,
          (2, 4, 1000, 8, 1, 16), (1, 31, 64, 2, 1, 80), (2, 33, 65, 3, 3, 32), (1, 127, 32, 4, 2, 64), (1, 130, 63, 2, 2, 112),
          (2, 129, 31, 6, 2, 96), (1, 300, 500, 2, 2, 128), (1, 257, 127, 8, 8, 16), (1, 1003, 129, 4, 1, 32),
          (1, 70, 2500, 1, 1, 64), (2, 2049, 40, 2, 2, 16), (1, 17_000, 70, 8, 8, 32), (1, 8500, 45, 16, 4, 64),
-         (1, 33_000, 33, 4, 4, 16)]
+         (1, 33_000, 33, 4, 4, 16), (2, 17_000, 97, 16, 16, 32), (1, 70_000, 40, 8, 4, 48)]
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
@@ -120,7 +123,7 @@ def test_cross_forward_and_backward(B, N, S, H, HK, D, dtype):
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("what", ["lengths", "mask", "both"])
 @pytest.mark.parametrize("B,N,S,H,HK,D", [(4, 3, 700, 4, 2, 32), (4, 200, 130, 2, 2, 16), (4, 150, 97, 4, 1, 64), (4, 40, 300, 2, 2, 128),
-                                          (4, 9000, 66, 4, 4, 32)])
+                                          (4, 9000, 66, 4, 4, 32), (4, 9000, 67, 16, 16, 16)])
 def test_cross_states_that_are_absent(B, N, S, H, HK, D, what, dtype):
     """Lengths of all, one, none and beyond the ends, masks with long runs and a sample of none; absent
     states hold infinities and not-a-numbers."""
