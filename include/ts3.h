@@ -612,10 +612,10 @@ ts3_status ts3_orth_free(ts3_orth *h);
 ts3_status ts3_orth_bytes(const ts3_orth *h, int64_t *bytes);
 
 /* 0 <= count <= 16384 tensors, sides up to 32768 (TS3_ERR_UNSUPPORTED beyond);
- * an empty tensor is skipped.  No two dst may overlap (INVALID_ARG); a dst may
- * overlap any src, as every source is read before the first result is written.
- * The workspace, about 8 (n + s) bytes for n elements and s = min(rows, cols)^2,
- * all padded to multiples of 64, grows with the calls. */
+ * an empty tensor is skipped.  No dst may overlap another tensor's src or dst, nor
+ * its own src in part (INVALID_ARG).  The workspace, about 8 (n + s) bytes for matrices beyond 64 x 64 of
+ * n elements and s = min(rows, cols)^2, padded to multiples of 64, grows with the
+ * calls. */
 ts3_status ts3_orth_matrices(ts3_orth *h, const ts3_matrix *matrices, int32_t count, void *stream);
 
 const char *ts3_status_string(ts3_status s);

@@ -204,7 +204,8 @@ class Orthogonalizer(_Handle):
 
     def __call__(self, updates, out=None):
         """The list of results, of each tensor's type (float32 or bfloat16) and shape: new tensors, or
-        those of the list `out`, which may be `updates` itself.  Results may not share memory."""
+        those of the list `out`, which may be `updates` itself.  A result may share no memory with
+        another tensor of either list."""
         if out is None:
             out = [torch.empty_like(t) for t in updates]
         table, device = self._table(updates, out)

@@ -116,6 +116,20 @@ template <typename All> int64_t cross_all(const CrossArgs &A, int64_t cus) {
     return blocks * bh < 4 * All::W * cus ? 0 : std::max<int64_t>(1, cus / bh);
 }
 
+// Tiles of a product and how many groups of waves share one, from the tiles of 128 and of 64 that there are.
+struct OrthShape {
+    int side, groups;
+};
+// A compute unit does one tile of 128 at a time: with one to four rounds of them, the last costs more than
+// smaller tiles do, and with fewer than half a round, idle units do.  On the GPU (256 units), 128 against 64: 1,536
+// tiles of 256 K 63 against 70 us, 432 of 256 to 1,024 K 44 against 39 and of 256 K 26 against 22, 144 of
+// 4,096 K 87 against 99, 1,024 of 1,024 K 136 against 174.  Few tiles of 64 have four groups of waves each
+// (18 of 512 K 7.4 against 9 us).
+OrthShape orth_shape(int64_t large, int64_t half, int64_t cus) {
+    if (large >= cus / 2 && (large <= cus || large >= 4 * cus)) return OrthShape{128, 1};
+    return OrthShape{64, half <= cus ? 4 : 1};
+}
+
 }  // namespace
 
 extern "C" {
@@ -453,7 +467,7 @@ ts3_status ts3_orth_matrices(ts3_orth *h, const ts3_matrix *matrices, int32_t co
     hipStream_t st = (hipStream_t)stream;
     try {
         std::vector<OrthEntry> list;
-        std::vector<std::pair<uintptr_t, uintptr_t>> to;
+        std::vector<ClipRun> runs;
         for (int32_t i = 0; i < count; ++i) {
             const ts3_matrix &m = matrices[i];
             if (!m.rows || !m.cols || !m.batch) continue;
@@ -465,72 +479,105 @@ ts3_status ts3_orth_matrices(ts3_orth *h, const ts3_matrix *matrices, int32_t co
             e.nb = m.batch;
             e.flags = (m.rows > m.cols ? ORTH_TURNED : 0) | (m.dtype == TS3_BF16 ? ORTH_BF16 : 0);
             list.push_back(e);
-            const int64_t size = (int64_t)m.rows * m.cols * m.batch * (m.dtype == TS3_BF16 ? 2 : 4);
-            to.emplace_back((uintptr_t)m.dst, (uintptr_t)m.dst + (uintptr_t)size);
+            runs.push_back(ClipRun{(const char *)m.src, (char *)m.dst, (int64_t)m.rows * m.cols * m.batch, m.dtype});
         }
-        if (list.empty()) return TS3_OK;
-        // Every source is read before the first result is written: only results may not overlap.
-        std::sort(to.begin(), to.end());
-        for (size_t i = 1; i < to.size(); ++i)
-            if (to[i].first < to[i - 1].second)
-                return fail(TS3_ERR_INVALID_ARG, "two results overlap (the same tensor twice, or views of one array)");
-        // Tiles of 128 where they fill the compute units twice, else of 64.
+        if (runs.empty()) return TS3_OK;
+        if (clip_overlaps(runs, true))
+            return fail(TS3_ERR_INVALID_ARG, "a result overlaps another tensor (the same one twice, or views of one array)");
+        // The longest sums first, and the small matrices behind the others.
+        std::stable_sort(list.begin(), list.end(), [](const OrthEntry &p, const OrthEntry &q) { return p.c > q.c; });
         const int64_t cus = device_cu_count();
         auto tiles = [](const OrthEntry &e, int ts, bool update) {
             const int64_t nr = (orth_pad(e.r) + ts - 1) / ts, nc = (orth_pad(e.c) + ts - 1) / ts;
-            return e.nb * (update ? nr * nc : nr * (nr + 1) / 2);
+            return e.c <= ORTH_SMALL ? 0 : e.nb * (update ? nr * nc : nr * (nr + 1) / 2);
         };
-        int64_t total[2] = {0, 0};
-        for (const OrthEntry &e : list)
-            for (int u : {0, 1}) total[u] += tiles(e, 128, u);
-        const int ts[2] = {total[0] >= 2 * cus ? 128 : 64, total[1] >= 2 * cus ? 128 : 64};
-        int64_t x = 0, a = 0, slack = 0, n[4] = {0, 0, 0, 0};
+        OrthShape shape[2];
+        for (int u : {0, 1}) {
+            int64_t large = 0, half = 0;
+            for (const OrthEntry &e : list) {
+                large += tiles(e, 128, u);
+                half += tiles(e, 64, u);
+            }
+            shape[u] = orth_shape(large, half, cus);
+        }
+        int64_t x = 0, a = 0, slack = 0, n[4] = {0, 0, 0, 0}, big = 0;
         for (OrthEntry &e : list) {
             const int64_t rp = orth_pad(e.r), cp = orth_pad(e.c);
+            const bool is_small = e.c <= ORTH_SMALL;
             e.x = x;
             e.a = a;
-            x += 2 * e.nb * rp * cp;
-            a += 2 * e.nb * rp * rp;
-            slack = std::max(slack, 64 * cp + 64);
             e.piece = (int32_t)n[0], e.load = (int32_t)n[1], e.gram = (int32_t)n[2], e.update = (int32_t)n[3];
-            n[0] += (int64_t)e.nb * orth_pieces((int64_t)e.r * e.c);
-            n[1] += e.nb * (rp / 64) * (cp / 64);
-            n[2] += tiles(e, ts[0], false);
-            n[3] += tiles(e, ts[1], true);
+            if (!is_small) {
+                x += 2 * e.nb * rp * cp;
+                a += 2 * e.nb * rp * rp;
+                slack = std::max(slack, 64 * cp + 64);
+            }
+            n[0] += is_small ? 1 : (int64_t)e.nb * orth_pieces((int64_t)e.r * e.c);
+            n[1] += is_small ? e.nb : e.nb * (rp / 64) * (cp / 64);
+            n[2] += tiles(e, shape[0].side, false);
+            n[3] += tiles(e, shape[1].side, true);
+            if (!is_small) big = n[1];
             for (int64_t k : n)
                 if (k >= int64_t(1) << 23) return fail(TS3_ERR_UNSUPPORTED, "no launch for so many or so large matrices");
         }
         auto align = [](int64_t v) { return (v + 255) & ~int64_t(255); };
-        const int64_t tb = align((int64_t)list.size() * (int64_t)sizeof(OrthEntry)), sb = align(n[0] * 8),
-                      xb = align((x + slack) * 2), ab = align((a + slack) * 2);
-        ts3_status s = h->work.reserve(tb + sb + 2 * xb + 2 * ab, st, h->bytes);
+        int64_t need = 0;
+        auto place = [&](int64_t bytes) {
+            const int64_t at = need;
+            need += align(bytes);
+            return at;
+        };
+        const int nl = (int)list.size();
+        const int64_t at_table = place((int64_t)nl * (int64_t)sizeof(OrthEntry)), at_sums = place(n[0] * 8);
+        const int64_t at_maps[3] = {place(n[1] * 4), place(n[2] * 4), place(n[3] * 4)};
+        const int64_t at_x[2] = {place((x + slack) * 2), place((x + slack) * 2)};
+        const int64_t at_a = place((a + slack) * 2), at_b = place((a + slack) * 2);
+        ts3_status s = h->work.reserve(need, st, h->bytes);
         if (s != TS3_OK) return s;
         unsigned char *const w = (unsigned char *)h->work.p;
-        OrthEntry *const table = (OrthEntry *)w;
-        double *const sums = (double *)(w + tb);
-        _Float16 *xs[2] = {(_Float16 *)(w + tb + sb), (_Float16 *)(w + tb + sb + xb)};
-        _Float16 *const as = (_Float16 *)(w + tb + sb + 2 * xb), *const bs = (_Float16 *)(w + tb + sb + 2 * xb + ab);
-        const int nl = (int)list.size();
+        OrthEntry *const table = (OrthEntry *)(w + at_table);
+        double *const sums = (double *)(w + at_sums);
+        _Float16 *const xs[2] = {(_Float16 *)(w + at_x[0]), (_Float16 *)(w + at_x[1])};
+        _Float16 *const as = (_Float16 *)(w + at_a), *const bs = (_Float16 *)(w + at_b);
+        OrthMaps maps{};
+        for (int k = 0; k < 3; ++k) maps.of[k] = (int32_t *)(w + at_maps[k]);
         for (int first = 0; first < nl; first += ORTH_BATCH) {
             OrthBatch b{};
             b.first = first;
             b.count = std::min(ORTH_BATCH, nl - first);
             std::copy(list.begin() + first, list.begin() + first + b.count, b.e);
-            const int64_t end = first + b.count < nl ? list[(size_t)(first + b.count)].piece : n[0];
-            hipLaunchKernelGGL(k_orth_norm, dim3((unsigned)(end - b.e[0].piece)), dim3(256), 0, st, b, table, sums);
+            const bool more = first + b.count < nl;
+            const OrthEntry &next = list[(size_t)(more ? first + b.count : 0)];
+            maps.end[ORTH_AT_LOAD] = more ? next.load : (int32_t)n[1];
+            maps.end[ORTH_AT_GRAM] = more ? next.gram : (int32_t)n[2];
+            maps.end[ORTH_AT_UPDATE] = more ? next.update : (int32_t)n[3];
+            const int64_t wgs = (more ? next.piece : n[0]) - b.e[0].piece;
+            hipLaunchKernelGGL(k_orth_norm, dim3((unsigned)wgs), dim3(256), 0, st, b, table, maps, sums);
             LAUNCH_CHECK("orthogonalisation norms");
         }
-        hipLaunchKernelGGL(k_orth_load, dim3((unsigned)n[1]), dim3(256), 0, st, table, nl, sums, (double)h->desc.eps, xs[0]);
+        const double eps = h->desc.eps;
+        if (n[1] > big) {
+            hipLaunchKernelGGL(k_orth_small, dim3((unsigned)(n[1] - big)), dim3(256), 0, st, table, maps.of[ORTH_AT_LOAD], (int)big,
+                               h->desc.steps, eps);
+            LAUNCH_CHECK("orthogonalisation of small matrices");
+        }
+        if (big == 0) return TS3_OK;
+        hipLaunchKernelGGL(k_orth_load, dim3((unsigned)big), dim3(256), 0, st, table, maps.of[ORTH_AT_LOAD], sums, eps, xs[0]);
         LAUNCH_CHECK("orthogonalisation operands");
-        const auto gram = ts[0] == 128 ? &k_orth_product<ORTH_GRAM, 128> : &k_orth_product<ORTH_GRAM, 64>;
-        const auto square = ts[0] == 128 ? &k_orth_product<ORTH_SQUARE, 128> : &k_orth_product<ORTH_SQUARE, 64>;
-        const auto update = ts[1] == 128 ? &k_orth_product<ORTH_UPDATE, 128> : &k_orth_product<ORTH_UPDATE, 64>;
+        auto product = [&](auto kind, const OrthShape &sh, int64_t count, const int32_t *map, const _Float16 *px, const _Float16 *pa,
+                           _Float16 *out, bool last) {
+            constexpr int KIND = decltype(kind)::value;
+            const auto kernel = sh.side == 128 ? &k_orth_stream<KIND> : sh.groups == 1 ? &k_orth_product<KIND, 64, 1> : &k_orth_product<KIND, 64, 4>;
+            const int64_t most = sh.side == 128 ? cus : sh.groups == 1 ? 4 * cus : count;
+            const int threads = sh.side == 128 ? 512 : 256 * sh.groups;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(count, most)), dim3(threads), 0, st, table, map, (int)count, px, pa, out,
+                               last);
+        };
         for (int i = 0; i < h->desc.steps; ++i) {
             const _Float16 *const from = xs[i & 1];
-            hipLaunchKernelGGL(gram, dim3((unsigned)n[2]), dim3(256), 0, st, table, nl, from, as, as, false);
-            hipLaunchKernelGGL(square, dim3((unsigned)n[2]), dim3(256), 0, st, table, nl, from, as, bs, false);
-            hipLaunchKernelGGL(update, dim3((unsigned)n[3]), dim3(256), 0, st, table, nl, from, bs, xs[i & 1 ^ 1],
-                               i + 1 == h->desc.steps);
+            product(ic<ORTH_GRAM>{}, shape[0], n[2], maps.of[ORTH_AT_GRAM], from, as, as, false);
+            product(ic<ORTH_SQUARE>{}, shape[0], n[2], maps.of[ORTH_AT_GRAM], from, as, bs, false);
+            product(ic<ORTH_UPDATE>{}, shape[1], n[3], maps.of[ORTH_AT_UPDATE], from, bs, xs[i & 1 ^ 1], i + 1 == h->desc.steps);
             LAUNCH_CHECK("orthogonalisation products");
         }
     } catch (const std::bad_alloc &) {

@@ -141,7 +141,7 @@ def _matrices(*rows):
 @pytest.mark.parametrize("row,status", [
     (dict(src=0), BAD), (dict(dst=0), BAD), (dict(src=MB + 2), BAD), (dict(dst=MB + 1, dtype=L.TS3_BF16), BAD),
     (dict(rows=-1), BAD), (dict(cols=-1), BAD), (dict(batch=-1), BAD), (dict(dtype=2), BAD), (dict(rows=32769), UNSUPPORTED),
-    (dict(cols=32769), UNSUPPORTED), (dict(batch=1 << 30), UNSUPPORTED),
+    (dict(cols=32769), UNSUPPORTED), (dict(batch=1 << 24, dst=1 << 40), UNSUPPORTED),
 ])
 def test_orth_refusals(row, status):
     assert L.lib().ts3_orth_matrices(_orth(), *_matrices(row), None) == status and L.lib().ts3_last_error()
@@ -149,7 +149,8 @@ def test_orth_refusals(row, status):
 
 def test_orth_results_that_overlap_and_empty_lists():
     lib, h = L.lib(), _orth()
-    for second in (dict(), dict(dst=64 * MB + 92), dict(src=2 * MB, dst=64 * MB - 4)):
+    for second in (dict(), dict(dst=64 * MB + 92), dict(src=2 * MB, dst=64 * MB - 4), dict(src=2 * MB, dst=MB + 92),
+                   dict(src=64 * MB + 92, dst=2 * MB), dict(src=2 * MB, dst=2 * MB + 4)):
         assert lib.ts3_orth_matrices(h, *_matrices(dict(), second), None) == BAD
     assert lib.ts3_orth_matrices(h, None, 0, None) == L.TS3_OK
     assert lib.ts3_orth_matrices(h, *_matrices(dict(rows=0), dict(batch=0, src=0, dst=0)), None) == L.TS3_OK
