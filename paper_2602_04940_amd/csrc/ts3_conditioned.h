@@ -205,16 +205,16 @@ ts3_status ts3_cross_forward(ts3_cross *h, const ts3_cross_inputs *in, void *out
         constexpr int P = decltype(p)::value, DP = decltype(dp)::value;
         const int64_t R = (int64_t)A.N * A.G, bh = (int64_t)A.B * HK, cus = device_cu_count();
         hipStream_t st = (hipStream_t)stream;
-        auto launch = [&](auto nq, auto w) -> ts3_status {
-            constexpr int NQ = decltype(nq)::value, W = decltype(w)::value, TK = cross_tile<P, DP, W>();
-            const int64_t blocks = (R + 32 * NQ * W - 1) / (32 * NQ * W), wgs = bh * blocks;
+        auto launch = [&](auto w) -> ts3_status {
+            constexpr int W = decltype(w)::value, TK = cross_tile<P, DP, W>();
+            const int64_t blocks = (R + 32 * W - 1) / (32 * W), wgs = bh * blocks;
             cross_split(A, blocks, (A.S + TK - 1) / TK, (W == 1 ? 8 : 2) * cus);
             if (A.splits > 1) {
                 ts3_status r = h->part.reserve(A.splits * bh * R * (DP + 4) * 4, st, h->bytes);
                 if (r != TS3_OK) return r;
                 A.part = (float *)h->part.p;
             }
-            hipLaunchKernelGGL((k_cross_fwd<P, DP, NQ, W>), dim3((unsigned)(wgs * A.splits)), dim3(64 * W), 0, st, A);
+            hipLaunchKernelGGL((k_cross_fwd<P, DP, W>), dim3((unsigned)(wgs * A.splits)), dim3(64 * W), 0, st, A);
             LAUNCH_CHECK("cross attention");
             if (A.splits > 1) {
                 hipLaunchKernelGGL((k_cross_join<P, DP>), dim3((unsigned)(bh * R)), dim3(256), 0, st, A);
@@ -224,7 +224,7 @@ ts3_status ts3_cross_forward(ts3_cross *h, const ts3_cross_inputs *in, void *out
         };
         // A wave of its own for a row or a few (float32 heads of 128 would not fit its registers).
         if constexpr (DP * P <= 192)
-            if (R <= 32) return launch(ic<1>{}, ic<1>{});
+            if (R <= 32) return launch(ic<1>{});
         using All = CrossAll<P, DP, 16>;
         if constexpr (All::FITS) if (const int64_t per = cross_all<All>(A, cus); per > 0) {
             if (ts3_status r = cross_allow_lds<P, DP>(h); r != TS3_OK) return r;
@@ -236,7 +236,7 @@ ts3_status ts3_cross_forward(ts3_cross *h, const ts3_cross_inputs *in, void *out
             LAUNCH_CHECK("cross attention");
             return TS3_OK;
         }
-        return launch(ic<1>{}, ic<4>{});
+        return launch(ic<4>{});
     });
 }
 
@@ -270,7 +270,7 @@ ts3_status ts3_cross_backward(ts3_cross *h, const ts3_cross_inputs *in, const vo
         CrossArgs Q = A, V = A;
         const int64_t qblocks = (R + 127) / 128, vblocks = (S + 127) / 128, qwgs = bh * qblocks, vwgs = bh * vblocks;
         cross_split(Q, qblocks, (S + T - 1) / T, 2 * cus);
-        using All = CrossAll<P, DP, 12>;
+        using All = CrossAll<P, DP, CROSS_DQ_WAVES<DP * P>>;
         const int64_t qall = cross_all<All>(A, cus);
         if (qall > 0) {
             Q.per = (int32_t)qall;
@@ -279,7 +279,7 @@ ts3_status ts3_cross_backward(ts3_cross *h, const ts3_cross_inputs *in, const vo
             Q.by_blocks = CrossDiv((uint32_t)qall);
         }
         cross_split(V, vblocks, (R + T - 1) / T, (DP * P <= 48 ? 3 : 2) * cus);
-        const int64_t qn = bh * R * DP, vn = states * D;
+        const int64_t qn = bh * R * (2 * DP + 4), vn = states * D;
         // one after the other: the parts share their memory
         const int64_t need = std::max(Q.splits > 1 ? Q.splits * qn * 4 : 0, V.splits > 1 ? 2 * V.splits * vn * 4 : 0);
         ts3_status r = h->part.reserve(need, st, h->bytes);
@@ -300,7 +300,7 @@ ts3_status ts3_cross_backward(ts3_cross *h, const ts3_cross_inputs *in, const vo
             hipLaunchKernelGGL((k_cross_dq<P, DP>), dim3((unsigned)(qwgs * Q.splits)), dim3(256), 0, st, Q);
             LAUNCH_CHECK("cross attention dq");
             if (Q.splits > 1) {
-                hipLaunchKernelGGL((k_cross_sum<P, DP, true>), dim3((unsigned)((qn + 255) / 256)), dim3(256), 0, st, Q, qn);
+                hipLaunchKernelGGL((k_cross_sum_dq<P, DP>), dim3((unsigned)((bh * R * DP + 255) / 256)), dim3(256), 0, st, Q, bh * R);
                 LAUNCH_CHECK("cross attention dq sums");
             }
         }
@@ -310,7 +310,7 @@ ts3_status ts3_cross_backward(ts3_cross *h, const ts3_cross_inputs *in, const vo
             hipLaunchKernelGGL((k_cross_dkv<P, DP>), dim3((unsigned)(vwgs * V.splits)), dim3(256), 0, st, V);
             LAUNCH_CHECK("cross attention dk and dv");
             if (V.splits > 1) {
-                hipLaunchKernelGGL((k_cross_sum<P, DP, false>), dim3((unsigned)((vn + 255) / 256), 2), dim3(256), 0, st, V, vn);
+                hipLaunchKernelGGL((k_cross_sum<typename GatedIO<P>::T>), dim3((unsigned)((vn + 255) / 256), 2), dim3(256), 0, st, V, vn);
                 LAUNCH_CHECK("cross attention dk and dv sums");
             }
         }

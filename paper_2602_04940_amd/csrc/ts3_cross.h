@@ -14,11 +14,11 @@
 // read once, and the sums over rows of dk and dv are over the group's heads too.
 //
 //   k_cross_fwd    scores, softmax with a running maximum and sum, and the weighted values, for
-//                  32 or 64 rows per wave against tiles of states in LDS
+//                  32 rows per wave against tiles of states in LDS
 //   k_cross_join   joins the parts of rows whose states were split over workgroups
 //   k_cross_dq     g.out and dq for 32 rows per wave, the scores computed again
 //   k_cross_dkv    dk and dv for 32 states per wave against tiles of rows in LDS
-//   k_cross_sum    sums of split gradients, in the splits' order
+//   k_cross_sum, k_cross_sum_dq   sums of split gradients, in the splits' order
 //
 // Products are 32x32x16 with the operand conventions of ts3_gated.h, bfloat16 as it is (P = 1),
 // float32 as three bfloat16 parts (P = 3).  Scores are computed transposed, rows the states in
@@ -302,182 +302,147 @@ __device__ __forceinline__ unsigned char cross_mask(const CrossArgs &A, int b, i
     return A.mask ? A.mask[(int64_t)b * A.S + (j < len ? j : 0)] : 1;
 }
 
-// The sum of the weights and their operand.  In bfloat16 the sum is of the rounded weights, which then add
-// to one: 0.5 vector instructions a weight instead of one.
-__device__ __forceinline__ float cross_weights(const float (&x)[8], Parts<1> &w, float sum) {
-    to_parts(x, w);
-    return sum_slots(w.p[0], sum);
-}
-__device__ __forceinline__ float cross_weights(const float (&x)[8], Parts<3> &w, float sum) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum += x[e];
-    to_parts(x, w);
-    return sum;
-}
-
-// 32 NQ rows of a wave on their way through the states.
+// 32 rows of a wave on their way through the states.
 //
 // The exponents are taken against a base per row, which need not be the maximum.  It is zero where the
 // row's first 32 states have a sum of weights of 2^-16 at least then, or else their maximum; afterwards
 // only what lies so far above that a lane's sum of 16 weights reaches 2^40 moves it.  The 32 states are
 // then done over, and the maximum is not looked for otherwise.  In float32 and bfloat16 the weights'
 // precision does not depend on the base.
-template <int P, int DP, int NQ> struct CrossRows {
+template <int P, int DP> struct CrossRows {
     using T = typename GatedIO<P>::T;
     using Score = CrossScore<P, DP>;
     static constexpr int KS = DP / 16, DB = (DP + 31) / 32;
-    Score qf[NQ];
-    f32x16 o[NQ][DB], start[NQ];  // start: minus the base, where the scores' accumulators begin
-    float base[NQ], l[NQ];
-    float low[NQ];  // what a sum has to reach: something while a row has no base yet, then nothing
+    Score qf;
+    f32x16 o[DB], start;  // start: minus the base, where the scores' accumulators begin
+    float base, l;
+    float low;  // what a sum has to reach: something while a row has no base yet, then nothing
 
-    // Rows r0 + 32 i, those past the last read as the last.
-    __device__ __forceinline__ void begin(const CrossArgs &A, const CrossAt &at, int r0) {
+    // Row r, one past the last read as the last.
+    __device__ __forceinline__ void begin(const CrossArgs &A, const CrossAt &at, int r) {
+        qf.load(cross_row<T>(A.q, A, at.b, at.hk, min(r, A.rows() - 1)), A.D, true, A.scale * LOG2E);
+        base = l = 0.f;
+        low = 0x1p-16f;
+        start = f32x16{};
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            qf[i].load(cross_row<T>(A.q, A, at.b, at.hk, min(r0 + 32 * i, A.rows() - 1)), A.D, true, A.scale * LOG2E);
-            base[i] = l[i] = 0.f;
-            low[i] = 0x1p-16f;
-            start[i] = f32x16{};
-#pragma unroll
-            for (int d = 0; d < DB; ++d) o[i][d] = f32x16{};
-        }
+        for (int d = 0; d < DB; ++d) o[d] = f32x16{};
     }
     // The states 32 u .. + 31 of a tile of keys and one of values; bit j of `here` is whether j is there.
     __device__ __forceinline__ void step(const unsigned char *kl, const unsigned char *vl, int plane, int u, uint32_t here,
                                          const CrossRowRead<DP> &rows, const CrossColRead<DP> &cols, float scale2, int g) {
         if (here == 0) return;
-        f32x16 s[NQ];
+        f32x16 s;
         // exponents against the base, absent states' at minus infinity
         auto scores = [&]() {
-#pragma unroll
-            for (int i = 0; i < NQ; ++i) s[i] = Score::PRE ? start[i] : f32x16{};
+            s = Score::PRE ? start : f32x16{};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 Parts<P> a;
                 rows.template read<P>(kl, plane, u, ks, a);
-#pragma unroll
-                for (int i = 0; i < NQ; ++i) qf[i].mma(s[i], a, ks);
+                qf.mma(s, a, ks);
             }
             if constexpr (!Score::PRE)
 #pragma unroll
-                for (int i = 0; i < NQ; ++i)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) s[i][v] = fmaf(s[i][v], scale2, -base[i]);
+                for (int v = 0; v < 16; ++v) s[v] = fmaf(s[v], scale2, -base);
             if (here != ~0u) {
                 uint32_t bits = here >> (16 * g);
                 asm("" : "+v"(bits));  // or the bits are taken apart where no state is absent, too
 #pragma unroll
-                for (int i = 0; i < NQ; ++i)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) s[i][v] = bits >> v & 1 ? s[i][v] : -INFINITY;
+                for (int v = 0; v < 16; ++v) s[v] = bits >> v & 1 ? s[v] : -INFINITY;
             }
         };
-        float sum[NQ];
-        Parts<P> w[NQ][2];
+        float sum;
+        Parts<P> w[2];
 #pragma unroll 1
         for (bool again = false;; again = true) {
             scores();
+            sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < NQ; ++i) {
-                sum[i] = 0.f;
+            for (int h = 0; h < 2; ++h) {
+                float x[8];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = fast_exp2(s[i][8 * h + e]);
-                    sum[i] = cross_weights(x, w[i][h], sum[i]);
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = fast_exp2(s[8 * h + e]);
+                    sum += x[e];
                 }
+                to_parts(x, w[h]);
             }
             if (again) break;
-            bool high = false;
-#pragma unroll
-            for (int i = 0; i < NQ; ++i) high = high || !(sum[i] < 0x1p40f && sum[i] >= low[i]);
-            if (!__any(high)) {
-#pragma unroll
-                for (int i = 0; i < NQ; ++i) low[i] = 0.f;
+            const unsigned out = !(sum < 0x1p40f && sum >= low);
+            if (!__any(out)) {
+                low = 0.f;
                 break;
             }
             scores();
+            // a row moves by its own sums alone: the others' results do not depend on it
+            const auto sw = __builtin_amdgcn_permlane32_swap(out, out, false, false);
+            const bool moves = sw[0] | sw[1], have = low == 0.f;
+            float mx = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < NQ; ++i) {
-                // a row moves by its own sums alone: the others' results do not depend on it
-                const unsigned out = !(sum[i] < 0x1p40f && sum[i] >= low[i]);
-                const auto sw = __builtin_amdgcn_permlane32_swap(out, out, false, false);
-                const bool moves = sw[0] | sw[1], have = low[i] == 0.f;
-                float mx = -INFINITY;
+            for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[v]);
+            const auto mw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+            mx = fmaxf(__uint_as_float(mw[0]), __uint_as_float(mw[1]));
+            const float up = !moves || mx == -INFINITY ? 0.f : have ? fmaxf(mx, 0.f) : mx;
+            const float alpha = have ? fast_exp2(-up) : 1.f;
+            if (!moves || mx > -INFINITY) low = 0.f;
+            base += up;
+            start = splat16(-base);
+            l *= alpha;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[i][v]);
-                const auto mw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-                mx = fmaxf(__uint_as_float(mw[0]), __uint_as_float(mw[1]));
-                const float up = !moves || mx == -INFINITY ? 0.f : have ? fmaxf(mx, 0.f) : mx;
-                const float alpha = have ? fast_exp2(-up) : 1.f;
-                if (!moves || mx > -INFINITY) low[i] = 0.f;
-                base[i] += up;
-                start[i] = splat16(-base[i]);
-                l[i] *= alpha;
-#pragma unroll
-                for (int d = 0; d < DB; ++d) o[i][d] *= alpha;
-            }
+            for (int d = 0; d < DB; ++d) o[d] *= alpha;
         }
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) l[i] += sum[i];
+        l += sum;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 Parts<P> a;
                 cols.template read<P>(vl, plane, u, h, d, a);
-#pragma unroll
-                for (int i = 0; i < NQ; ++i) mma_parts<32, P>(o[i][d], a, w[i][h]);
+                mma_parts<32, P>(o[d], a, w[h]);
             }
     }
-    __device__ __forceinline__ void finish(const CrossArgs &A, const CrossAt &at, int r0, int g) const {
+    __device__ __forceinline__ void finish(const CrossArgs &A, const CrossAt &at, int r, int g) const {
         const int R = A.rows();
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+        const float sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+        if (r >= R) return;
+        if (A.splits == 1) {
+            // no state: weights of zero, whose sum is minus infinity in the logarithm
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            T *const to = cross_to((T *)A.to, A, at.b, at.hk, r);
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            const int r = r0 + 32 * i;
-            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[i]), __float_as_uint(l[i]), false, false);
-            const float sum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-            if (r >= R) continue;
-            if (A.splits == 1) {
-                // no state: weights of zero, whose sum is minus infinity in the logarithm
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                T *const to = cross_to((T *)A.to, A, at.b, at.hk, r);
+            for (int d = 0; d < DB; ++d) {
+                const int c = 32 * d + 16 * g;
+                float x[16];
 #pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const int c = 32 * d + 16 * g;
-                    float x[16];
+                for (int v = 0; v < 16; ++v) x[v] = o[d][v] * inv;
+                if (c < A.D) store_row<16>(to + c, x);
+            }
+            if (g == 0) *cross_stat(A.lse, A, at.b, at.hk, r) = sum == 0.f ? -INFINITY : (base + log2f(sum)) * LN2;
+        } else {
+            // part[split][b][hk][r][DP + 4]: unscaled sums, their base and their weights' sum
+            const int64_t row = (((int64_t)at.split * A.B + at.b) * A.heads() + at.hk) * R + r;
+            float *const to = A.part + row * (DP + 4);
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) x[v] = o[i][d][v] * inv;
-                    if (c < A.D) store_row<16>(to + c, x);
-                }
-                if (g == 0) *cross_stat(A.lse, A, at.b, at.hk, r) = sum == 0.f ? -INFINITY : (base[i] + log2f(sum)) * LN2;
-            } else {
-                // part[split][b][hk][r][DP + 4]: unscaled sums, their base and their weights' sum
-                const int64_t row = (((int64_t)at.split * A.B + at.b) * A.heads() + at.hk) * R + r;
-                float *const to = A.part + row * (DP + 4);
+            for (int d = 0; d < DB; ++d) {
+                const int c = 32 * d + 16 * g;
+                float x[16];
 #pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const int c = 32 * d + 16 * g;
-                    float x[16];
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) x[v] = o[i][d][v];
-                    if (c < A.D) store_row<16>(to + c, x);
-                }
-                if (g == 0) {
-                    to[DP] = sum == 0.f ? -INFINITY : base[i];
-                    to[DP + 1] = sum;
-                }
+                for (int v = 0; v < 16; ++v) x[v] = o[d][v];
+                if (c < A.D) store_row<16>(to + c, x);
+            }
+            if (g == 0) {
+                to[DP] = sum == 0.f ? -INFINITY : base;
+                to[DP + 1] = sum;
             }
         }
     }
 };
 
-// Workgroup (b, hk, block, split): 32 NQ rows per wave, W waves, against the split's tiles of
+// Workgroup (b, hk, block, split): 32 rows per wave, W waves, against the split's tiles of
 // states.  The next tile is on its way to registers while this one is used, and goes to the other
 // half of LDS after it (a wave alone needs one half: its own reads come first).
-template <int P, int DP, int NQ, int W>
+template <int P, int DP, int W>
 __global__ __launch_bounds__(64 * W, W == 4 ? (DP * P <= 32 ? 4 : DP * P <= 96 ? 2 : 1) : 1) void k_cross_fwd(const CrossArgs A) {
     using T = typename GatedIO<P>::T;
     constexpr int TK = cross_tile<P, DP, W>(), SUB = TK / 32, HALVES = W == 1 ? 1 : 2;
@@ -487,10 +452,10 @@ __global__ __launch_bounds__(64 * W, W == 4 ? (DP * P <= 32 ? 4 : DP * P <= 96 ?
     const CrossAt at(A);
     const int len = cross_length(A, at.b), tiles = (len + TK - 1) / TK;
     const int t0 = at.split * A.per, t1 = min(tiles, t0 + A.per);
-    const int r0 = (at.blk * W + wave) * 32 * NQ + (lane & 31);
+    const int r0 = (at.blk * W + wave) * 32 + (lane & 31);
     const T *const kb = (const T *)A.k.p + at.b * A.k.sb + at.hk * A.k.sh;
     const T *const vb = (const T *)A.v.p + at.b * A.v.sb + at.hk * A.v.sh;
-    CrossRows<P, DP, NQ> q;
+    CrossRows<P, DP> q;
     q.begin(A, at, r0);
     const CrossRowRead<DP> rows(lane);
     const CrossColRead<DP> cols(lane);
@@ -598,7 +563,7 @@ __global__ __launch_bounds__(1024, 4) void k_cross_fwd_all(const CrossArgs A) {
     const CrossColRead<DP> cols(lane);
     for (int64_t first; (first = All::next(A, at, taken)) < R;) {
         const int r0 = (int)first;
-        CrossRows<P, DP, 1> q;
+        CrossRows<P, DP> q;
         q.begin(A, at, r0 + (lane & 31));
         for (int t = 0; t < n; ++t) {
             const uint64_t there = present[t];
@@ -655,15 +620,24 @@ template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_join(con
     if (tid == 0) *cross_stat(A.lse, A, b, hk, r) = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
 }
 
-// 32 rows of a wave: delta = g.out, and dq from the states they go through, the values being a second
-// operand of rows and the keys read transposed.
+// 32 rows of a wave: dq from the states they go through, the values being a second operand of rows and the
+// keys read transposed, and delta = g.out.
+//
+// In bfloat16 out is rounded, and delta from it is off by 2^-8 of |g| |out|, which where a row's weight lies on few
+// states is much of dp - delta.  It is what the slopes start from, but the loop takes sum p dp, which is
+// delta, in float32 and sum p k beside it, and dq is put right at the end by their difference; dk is
+// computed from the better delta (250,001 points of 512 states of width 32: dq off by 0.0026 of its
+// size before, by 0.0024 with it, and by 0.0017 of that from its own rounding).
 template <int P, int DP> struct CrossSlopes {
     using T = typename GatedIO<P>::T;
     using Score = CrossScore<P, DP>;
     static constexpr int KS = DP / 16, DB = (DP + 31) / 32;
+    static constexpr bool MEND = P == 1;
     Score qf;
     Parts<P> gf[KS];
-    f32x16 o[DB], start, dstart;  // minus the logarithm of the sum, and minus delta
+    f32x16 o[DB], start, dstart;  // minus the logarithm of the sum, and minus delta from out
+    f32x16 means[MEND ? DB : 1];  // sum p k
+    float rest;                   // of the lane's states, sum p (dp - delta from out)
     __device__ __forceinline__ void begin(const CrossArgs &A, const CrossAt &at, int r, int g) {
         const int rc = min(r, A.rows() - 1), D = A.D;
         const T *const grow = cross_row<T>(A.g, A, at.b, at.hk, rc), *const orow = cross_row<T>(A.out, A, at.b, at.hk, rc);
@@ -682,11 +656,14 @@ template <int P, int DP> struct CrossSlopes {
         }
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(delta), __float_as_uint(delta), false, false);
         delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-        if (r < A.rows() && g == 0 && at.split == 0) *cross_stat(A.delta, A, at.b, at.hk, r) = delta;
         start = splat16(-LOG2E * *cross_stat(A.lse, A, at.b, at.hk, rc));
         dstart = splat16(-delta);
 #pragma unroll
-        for (int d = 0; d < DB; ++d) o[d] = f32x16{};
+        for (int d = 0; d < DB; ++d) {
+            o[d] = f32x16{};
+            if constexpr (MEND) means[d] = f32x16{};
+        }
+        rest = 0.f;
     }
     __device__ __forceinline__ void step(const unsigned char *kl, const unsigned char *vl, int plane, int u, uint32_t here,
                                          const CrossRowRead<DP> &rows, const CrossColRead<DP> &cols, float scale2, int g) {
@@ -701,42 +678,70 @@ template <int P, int DP> struct CrossSlopes {
             mma_parts<32, P>(dp, a, gf[ks]);
         }
 #pragma unroll
-        for (int v = 0; v < 16; ++v) s[v] = fast_exp2(Score::PRE ? s[v] : fmaf(s[v], scale2, start[0])) * dp[v];
+        for (int v = 0; v < 16; ++v) s[v] = fast_exp2(Score::PRE ? s[v] : fmaf(s[v], scale2, start[0]));
         if (here != ~0u) {
             uint32_t bits = here >> (16 * g);
             asm("" : "+v"(bits));
 #pragma unroll
-            for (int v = 0; v < 16; ++v) s[v] = bits >> v & 1 ? s[v] : 0.f;
+            for (int v = 0; v < 16; ++v) {
+                s[v] = bits >> v & 1 ? s[v] : 0.f;
+                dp[v] = bits >> v & 1 ? dp[v] : 0.f;
+            }
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float x[8];
+            float x[8], y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = s[8 * h + e];
-            Parts<P> w;
+            for (int e = 0; e < 8; ++e) {
+                y[e] = s[8 * h + e];
+                x[e] = y[e] * dp[8 * h + e];
+                if constexpr (MEND) rest += x[e];
+            }
+            Parts<P> w, z;
             to_parts(x, w);
+            if constexpr (MEND) to_parts(y, z);
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 Parts<P> a;
                 cols.template read<P>(kl, plane, u, h, d, a);
                 mma_parts<32, P>(o[d], a, w);
+                if constexpr (MEND) mma_parts<32, P>(means[d], a, z);
             }
         }
     }
+    // Parts of split loops hold sum p (dp - delta from out) k, that of p k and that without k, a row of 2 DP + 4.
     __device__ __forceinline__ void finish(const CrossArgs &A, const CrossAt &at, int r, int g) const {
         const int R = A.rows();
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(rest), __float_as_uint(rest), false, false);
+        const float off = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
         if (r >= R) return;
-        float *const part = A.part + ((((int64_t)at.split * A.B + at.b) * A.heads() + at.hk) * R + r) * DP;
+        float *const part = A.part + ((((int64_t)at.split * A.B + at.b) * A.heads() + at.hk) * R + r) * (2 * DP + 4);
         T *const to = cross_to((T *)A.to, A, at.b, at.hk, r);
+        if (g == 0) {
+            if (A.splits == 1 || at.split == 0) *cross_stat(A.delta, A, at.b, at.hk, r) = (A.splits == 1 ? off : 0.f) - dstart[0];
+            if (A.splits > 1) part[2 * DP] = off;
+        }
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
             const int c = 32 * d + 16 * g;
             float x[16];
 #pragma unroll
-            for (int v = 0; v < 16; ++v) x[v] = o[d][v] * A.scale;
-            if (c < A.D) {
-                if (A.splits == 1) store_row<16>(to + c, x);
-                else store_row<16>(part + c, x);
+            for (int v = 0; v < 16; ++v) {
+                x[v] = o[d][v];
+                if constexpr (MEND)
+                    if (A.splits == 1) x[v] -= off * means[d][v];
+                x[v] *= A.splits == 1 ? A.scale : 1.f;
+            }
+            if (c >= A.D) continue;
+            if (A.splits == 1) {
+                store_row<16>(to + c, x);
+                continue;
+            }
+            store_row<16>(part + c, x);
+            if constexpr (MEND) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) x[v] = means[d][v];
+                store_row<16>(part + DP + c, x);
             }
         }
     }
@@ -799,9 +804,12 @@ template <int P, int DP> __global__ __launch_bounds__(256, DP * P <= 96 ? 2 : 1)
     }
     q.finish(A, at, r, g);
 }
+// As many waves as the registers allow: with sum p k, bfloat16 heads of 64 spill at 12 (the whole gradient of
+// 100,003 points of 256 states and 4 heads 277 us, at 8 waves 211).
+template <int WIDTH> constexpr int CROSS_DQ_WAVES = WIDTH <= 48 ? 12 : 8;
 template <int P, int DP>
-__global__ __launch_bounds__(768, 3) void k_cross_dq_all(const CrossArgs A) {
-    using All = CrossAll<P, DP, 12>;
+__global__ __launch_bounds__(64 * CROSS_DQ_WAVES<DP * P>, CROSS_DQ_WAVES<DP * P> / 4) void k_cross_dq_all(const CrossArgs A) {
+    using All = CrossAll<P, DP, CROSS_DQ_WAVES<DP * P>>;
     extern __shared__ __align__(16) unsigned char all_lds[];
     const CrossAt at(A);
     const int lane = threadIdx.x & 63, g = lane >> 5, R = A.rows();
@@ -973,27 +981,36 @@ template <int P, int DP> __global__ __launch_bounds__(256, DP * P <= 64 ? 2 : 1)
     }
 }
 
-// out[i] = the splits' values of element i, in order.  Of dq the parts lie [b][hk][r][DP], of dk and dv as
-// the results do.
-template <int P, int DP, bool DQ> __global__ __launch_bounds__(256) void k_cross_sum(const CrossArgs A, int64_t count) {
-    using T = typename GatedIO<P>::T;
+// dk and dv: the splits' values of element i, in order.
+template <typename T> __global__ __launch_bounds__(256) void k_cross_sum(const CrossArgs A, int64_t count) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= count) return;
-    if constexpr (DQ) {
-        const int64_t bhr = i / DP;
-        const int c = (int)(i % DP), R = A.rows();
-        if (c >= A.D) return;
-        float v = 0.f;
+    const float *const p = blockIdx.y ? A.part2 : A.part;
+    float v = 0.f;
 #pragma unroll 8
-        for (int s = 0; s < A.splits; ++s) v += A.part[s * count + i];
-        cross_to((T *)A.to, A, (int)(bhr / R / A.heads()), (int)(bhr / R % A.heads()), (int)(bhr % R))[c] = from_float<T>(v);
-    } else {
-        const float *const p = blockIdx.y ? A.part2 : A.part;
-        float v = 0.f;
+    for (int s = 0; s < A.splits; ++s) v += p[s * count + i];
+    ((T *)(blockIdx.y ? A.to2 : A.to))[i] = from_float<T>(v);
+}
+// dq from the splits' parts, in order, and delta: DP threads a row.
+template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_sum_dq(const CrossArgs A, int64_t count) {
+    using T = typename GatedIO<P>::T;
+    const int64_t bhr = ((int64_t)blockIdx.x * 256 + threadIdx.x) / DP;
+    const int c = threadIdx.x % DP, R = A.rows();
+    if (bhr >= count || c >= A.D) return;
+    const float *const p = A.part + bhr * (2 * DP + 4);
+    const int64_t step = count * (2 * DP + 4);
+    float v = 0.f, m = 0.f, off = 0.f;
 #pragma unroll 8
-        for (int s = 0; s < A.splits; ++s) v += p[s * count + i];
-        ((T *)(blockIdx.y ? A.to2 : A.to))[i] = from_float<T>(v);
+    for (int s = 0; s < A.splits; ++s) {
+        v += p[s * step + c];
+        if constexpr (P == 1) {
+            m += p[s * step + DP + c];
+            off += p[s * step + 2 * DP];
+        }
     }
+    const int b = (int)(bhr / R / A.heads()), hk = (int)(bhr / R % A.heads()), r = (int)(bhr % R);
+    cross_to((T *)A.to, A, b, hk, r)[c] = from_float<T>(A.scale * (v - off * m));
+    if (P == 1 && c == 0) *cross_stat(A.delta, A, b, hk, r) += off;
 }
 
 }  // namespace ts3

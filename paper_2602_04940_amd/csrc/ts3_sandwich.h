@@ -208,7 +208,9 @@ __global__ __launch_bounds__(256) void k_sandwich_bwd(const SandwichGrads<T> A, 
 #pragma unroll
             for (int i = 0; i < V; ++i) s[j][k][i] = 0.f;
     const int64_t step = (int64_t)gridDim.x * 4 * RW;
-    // the next row's loads go out before this row's arithmetic
+    // The next row's loads go out before this row's arithmetic, in bfloat16: float32, with half the arithmetic a
+    // byte, waits for memory anyway, and loses to more registers (2M rows of 128 1.18 against 1.34 ms).
+    constexpr bool EARLY = sizeof(T) == 2;
     RawPiece<T, V> rf[K], rd[K], ra[K], ry[K], re[K];
     auto fetch = [&](int64_t r0) {
         const int64_t row = r0 + lane / LG, at = (row < A.n ? row : A.n - 1) * C;
@@ -221,12 +223,13 @@ __global__ __launch_bounds__(256) void k_sandwich_bwd(const SandwichGrads<T> A, 
         }
     };
     const int64_t first = ((int64_t)blockIdx.x * 4 + wave) * RW;
-    if (first < A.n) fetch(first);
+    if (EARLY && first < A.n) fetch(first);
     for (int64_t r0 = first; r0 < A.n; r0 += step) {
         const int64_t row = r0 + lane / LG;
         const bool live = row < A.n;
         const int64_t at = (live ? row : A.n - 1) * C;
         float v[K][V], w[K][V], d[K][V], e[K][V], a[K][V];
+        if constexpr (!EARLY) fetch(r0);
         cols.get(A.f, rf, v);
         cols.get(A.gy, rd, d);
         cols.get(A.gate, ra, a);
@@ -234,7 +237,7 @@ __global__ __launch_bounds__(256) void k_sandwich_bwd(const SandwichGrads<T> A, 
             cols.get(A.y, ry, w);
             cols.get(A.gn, re, e);
         }
-        if (r0 + step < A.n) fetch(r0 + step);
+        if (EARLY && r0 + step < A.n) fetch(r0 + step);
         if (A.gn) {
             const float rs = norm_stats<LG, K, V>(w, cols.in, (float)C, A.eps);
 #pragma unroll
@@ -302,9 +305,9 @@ struct SandwichSums {
     float *to[SANDWICH_SUMS];
 };
 __global__ __launch_bounds__(256) void k_sandwich_join(const float *__restrict__ part, int nblk, int C, const SandwichSums d) {
-    __shared__ float s[16][17];
+    __shared__ double s[16][17];
     const int c = threadIdx.x & 15, q = threadIdx.x >> 4, at = blockIdx.x * 16 + c;
-    float v = 0.f;
+    double v = 0.0;
 #pragma unroll 8
     for (int b = q; b < nblk; b += 16) v += part[(int64_t)b * SANDWICH_SUMS * C + at];
     s[q][c] = v;
@@ -312,7 +315,7 @@ __global__ __launch_bounds__(256) void k_sandwich_join(const float *__restrict__
     if (q) return;
     for (int i = 1; i < 16; ++i) v += s[i][c];
     float *const to = d.to[at / C];
-    if (to) to[at % C] = v;
+    if (to) to[at % C] = (float)v;
 }
 
 }  // namespace ts3

@@ -8,12 +8,9 @@ Attention.  A score is a sum of D products of operands carried to u: it is off b
 X = scale |q| |k| at its largest, and so is its weight, relative to itself.  Sums over S states and N
 points walk their square roots.  In float32 every output is then within four times
 (8 + sqrt S + sqrt N + (4 + sqrt D) X) u of the size of its terms (the sum of their absolute values).
-In bfloat16 the output is rounded once (2^-8 of itself), and so are its weights p.  Their sum is of the
-rounded ones: with p (1 + e), |e| <= 2^-8, the output is off by sum p e (v - out) / sum p (1 + e), at most 2^-8 of
-the size of its terms and 2^-8 of itself again, and lse by log(1 + 2^-8).  The backward's p are off by as much
-before they are rounded: dv is within 2^-8 of itself and twice 2^-8 of its size.  dq and dk take slopes that
-are rounded (2^-8 of their size), of such p (again), and g.out from the rounded output (again: the
-reference's sizes hold both g.v and g.out), whose own weights were rounded (again).
+In bfloat16 the output is rounded once (2^-8 of itself), and so are its weights (2^-8 of the size of its
+terms); so is dv.  dq and dk take slopes that are rounded (2^-8 of their size) after g.out was put right; before it
+was from the rounded output, whose weights were rounded (again twice, which the reference's sizes hold).
 
 Norms.  As the other training operators': four walks over C, and over N for sums over rows, of the
 largest value in float32; in bfloat16 2^-8 in the mean square.
@@ -57,7 +54,7 @@ def _check(name, got, ref, size, dtype, walk):
     if ref.size == 0:
         return
     assert np.isfinite(got).all(), name
-    err, (own, rounds) = np.abs(got - ref), {"out": (2, 1), "dv": (1, 2), "dq": (1, 4), "dk": (1, 4)}[name]
+    err, (own, rounds) = np.abs(got - ref), {"out": (1, 1), "dv": (1, 1), "dq": (1, 3), "dk": (1, 3)}[name]
     bar = 4 * walk * U * size.max()
     if dtype == "bf16":
         bar = bar + 2.0 ** -8 * (own * np.abs(ref) + rounds * 1.02 * size)
@@ -93,7 +90,7 @@ def _compare(q, k, v, g, dtype, there, scale, out, lse, grads):
     empty = np.isinf(ref_lse)
     got = to_host(lse)
     assert (got[empty] == -np.inf).all()
-    assert np.abs(got[~empty] - ref_lse[~empty]).max(initial=0.0) <= 4 * walk * U * (1 + X) + (2.0 ** -8 if dtype == "bf16" else 0)
+    assert np.abs(got[~empty] - ref_lse[~empty]).max(initial=0.0) <= 4 * walk * U * (1 + X)
     for name in ("dq", "dk", "dv"):
         _check(name, grads[name], refs[name], sizes[name], dtype, walk)
         if name != "dq":
