@@ -208,7 +208,8 @@ ts3_status ts3_cross_forward(ts3_cross *h, const ts3_cross_inputs *in, void *out
         auto launch = [&](auto w) -> ts3_status {
             constexpr int W = decltype(w)::value, TK = cross_tile<P, DP, W>();
             const int64_t blocks = (R + 32 * W - 1) / (32 * W), wgs = bh * blocks;
-            cross_split(A, blocks, (A.S + TK - 1) / TK, (W == 1 ? 8 : 2) * cus);
+            // as many workgroups as fit: 30,000 rows of width 32 against 2,782 states 67 us with two a unit, 37 with four
+            cross_split(A, blocks, (A.S + TK - 1) / TK, (W == 1 ? 8 : DP * P <= 32 ? 4 : 2) * cus);
             if (A.splits > 1) {
                 ts3_status r = h->part.reserve(A.splits * bh * R * (DP + 4) * 4, st, h->bytes);
                 if (r != TS3_OK) return r;
@@ -217,7 +218,12 @@ ts3_status ts3_cross_forward(ts3_cross *h, const ts3_cross_inputs *in, void *out
             hipLaunchKernelGGL((k_cross_fwd<P, DP, W>), dim3((unsigned)(wgs * A.splits)), dim3(64 * W), 0, st, A);
             LAUNCH_CHECK("cross attention");
             if (A.splits > 1) {
-                hipLaunchKernelGGL((k_cross_join<P, DP>), dim3((unsigned)(bh * R)), dim3(256), 0, st, A);
+                const int64_t count = bh * R, few = (count * (DP / 4) + 255) / 256;
+                // 12,496 rows of width 80 in two parts: 67 us in all with a workgroup a row, 45 with lanes
+                if (A.splits <= 16 && few >= cus)
+                    hipLaunchKernelGGL((k_cross_join_few<P, DP>), dim3((unsigned)few), dim3(256), 0, st, A, count);
+                else
+                    hipLaunchKernelGGL((k_cross_join<P, DP>), dim3((unsigned)count), dim3(256), 0, st, A);
                 LAUNCH_CHECK("cross attention join");
             }
             return TS3_OK;

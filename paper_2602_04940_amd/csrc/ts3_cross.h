@@ -15,7 +15,7 @@
 //
 //   k_cross_fwd    scores, softmax with a running maximum and sum, and the weighted values, for
 //                  32 rows per wave against tiles of states in LDS
-//   k_cross_join   joins the parts of rows whose states were split over workgroups
+//   k_cross_join, k_cross_join_few   join the parts of rows whose states were split over workgroups
 //   k_cross_dq     g.out and dq for 32 rows per wave, the scores computed again
 //   k_cross_dkv    dk and dv for 32 states per wave against tiles of rows in LDS
 //   k_cross_sum, k_cross_sum_dq   sums of split gradients, in the splits' order
@@ -576,8 +576,34 @@ __global__ __launch_bounds__(1024, 4) void k_cross_fwd_all(const CrossArgs A) {
     }
 }
 
-// A row per workgroup: the splits' parts scaled to the largest base and added, 1024 / DP splits at a
-// time by as many groups of lanes, then the groups' sums in order.
+// Few parts: a row per DP / 4 lanes, which take the splits' parts in order, scaled to the largest base.
+template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_join_few(const CrossArgs A, int64_t count) {
+    using T = typename GatedIO<P>::T;
+    constexpr int LG = DP / 4;
+    const int64_t bhr = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LG, step = count * (DP + 4);
+    const int c = 4 * (threadIdx.x % LG), R = A.rows();
+    if (bhr >= count || c >= A.D) return;
+    const float *const part = A.part + bhr * (DP + 4);
+    float top = -INFINITY;
+    for (int s = 0; s < A.splits; ++s) top = fmaxf(top, part[s * step + DP]);
+    const float base = top == -INFINITY ? 0.f : top;
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < A.splits; ++s) {
+        const float *const p = part + s * step;
+        const float w = fast_exp2(p[DP] - base);
+        v += w * *reinterpret_cast<const f32x4 *>(p + c);
+        sum += w * p[DP + 1];
+    }
+    const int b = (int)(bhr / R / A.heads()), hk = (int)(bhr / R % A.heads()), r = (int)(bhr % R);
+    T *const to = cross_to((T *)A.to, A, b, hk, r) + c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to[i] = from_float<T>(sum == 0.f ? 0.f : v[i] / sum);
+    if (c == 0) *cross_stat(A.lse, A, b, hk, r) = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
+}
+// Many: a row per workgroup, 1024 / DP splits at a time by as many groups of lanes, then the groups' sums in
+// order.
 template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_join(const CrossArgs A) {
     using T = typename GatedIO<P>::T;
     constexpr int LG = DP / 4, NG = 256 / LG;
