@@ -501,7 +501,9 @@ ts3_status ts3_clip_gradients(ts3_clip *h, const ts3_clip_tensor *tensors, int32
  *  io_dtype: ts3_dtype of q, k, v, out and their gradients.  TS3_BF16 computes
  *            on bf16 matrix cores with float32 sums and rounds p (and, in the
  *            backward, p and ds) to bfloat16 once; TS3_FP32 keeps every operand to
- *            float32 precision in three bf16 parts.
+ *            float32 precision in three bf16 parts.  Weights are held against a
+ *            base of up to 2^40 below their sum, so that values beyond 2^64 may
+ *            overflow.
  *  scale   : finite and > 0; 0 stands for 1 / sqrt(D). */
 typedef struct {
     int32_t H, Hkv, D;
@@ -535,8 +537,9 @@ typedef struct {
  * overlap no input (TS3_ERR_INVALID_ARG).  S = 0 is allowed; B = 0 or N = 0 is a
  * no-op.  TS3_ERR_UNSUPPORTED where N * H / Hkv or S reaches 2^31 - 1024, or a
  * launch 2^24 workgroups (of 32 to 256 rows).  Few points split the states over
- * workgroups, whose parts are joined in a fixed order; the parts' workspace grows
- * with the calls, as the store of ts3_gated_backward does. */
+ * workgroups, whose parts are joined in a fixed order: results repeat bitwise for
+ * given sizes.  The parts' workspace grows with the calls, as the store of
+ * ts3_gated_backward does. */
 ts3_status ts3_cross_forward(ts3_cross *h, const ts3_cross_inputs *in, void *out, float *lse, void *stream);
 
 /* Gradients of sum(g * out) for the forward's inputs, out and lse: dq as out, dk
@@ -611,11 +614,12 @@ ts3_status ts3_orth_create(const ts3_orth_desc *desc, ts3_orth **out);
 ts3_status ts3_orth_free(ts3_orth *h);
 ts3_status ts3_orth_bytes(const ts3_orth *h, int64_t *bytes);
 
-/* 0 <= count <= 16384 tensors, sides up to 32768 (TS3_ERR_UNSUPPORTED beyond);
- * an empty tensor is skipped.  No dst may overlap another tensor's src or dst, nor
- * its own src in part (INVALID_ARG).  The workspace, about 8 (n + s) bytes for matrices beyond 64 x 64 of
- * n elements and s = min(rows, cols)^2, padded to multiples of 64, grows with the
- * calls. */
+/* 0 <= count <= 16384 tensors, sides up to 32768, 2^40 elements a tensor and 2^23
+ * tiles of work in all (TS3_ERR_UNSUPPORTED beyond); an empty tensor is
+ * skipped.  No dst may overlap another tensor's src or dst, nor its own src in
+ * part (INVALID_ARG).  The workspace, about 8 (n + s) bytes for matrices beyond
+ * 64 x 64 of n elements and s = min(rows, cols)^2, padded to multiples of 64,
+ * grows with the calls. */
 ts3_status ts3_orth_matrices(ts3_orth *h, const ts3_matrix *matrices, int32_t count, void *stream);
 
 const char *ts3_status_string(ts3_status s);

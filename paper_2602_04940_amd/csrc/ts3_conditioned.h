@@ -494,6 +494,8 @@ ts3_status ts3_orth_matrices(ts3_orth *h, const ts3_matrix *matrices, int32_t co
         if (!m.rows || !m.cols || !m.batch) continue;
         if (m.rows > SIDE || m.cols > SIDE)
             return fail(TS3_ERR_UNSUPPORTED, "tensor %d: no kernel for a %d x %d matrix (sides up to %d)", i, m.rows, m.cols, SIDE);
+        if ((int64_t)m.rows * m.cols > (int64_t(1) << 40) / m.batch)
+            return fail(TS3_ERR_UNSUPPORTED, "tensor %d: no launch for so many or so large matrices", i);
         const uintptr_t type = m.dtype == TS3_BF16 ? 1 : 3;
         if (!m.src || !m.dst || (((uintptr_t)m.src | (uintptr_t)m.dst) & type))
             return fail(TS3_ERR_INVALID_ARG, "tensor %d: a pointer is NULL or not aligned to its type", i);

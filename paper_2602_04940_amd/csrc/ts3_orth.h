@@ -333,6 +333,11 @@ __device__ __forceinline__ void orth_write(const OrthJob<KIND, TS> &job, const f
 // registers and one in each half of LDS, those of the next tile asked for before this one is written.
 // Where tiles are few, GROUPS groups of four waves each take every GROUPS-th pair of steps of one tile (the
 // grid then has a workgroup for each), and the first adds their sums in order.
+//
+// The three products of six matrices of 128 x 128 to 512 take 7, 5 and 5 us, a launch's and a chain of loads'
+// latency; those of 144 of 256 x 256 to 1024 39 and 22 us (k_orth_stream has the third: 62), with matrix cores on
+// 33 and 24% of the cycles: of a tile's four to sixteen pairs of steps the first waits for memory and an
+// epilogue follows the last.
 template <int KIND, int TS, int GROUPS>
 __global__ __launch_bounds__(256 * GROUPS, TS == 64 ? 4 : 2) void k_orth_product(const OrthEntry *__restrict__ table, const int32_t *__restrict__ map,
                                                       int tiles, const _Float16 *__restrict__ xs,
@@ -470,7 +475,7 @@ __global__ __launch_bounds__(256 * GROUPS, TS == 64 ? 4 : 2) void k_orth_product
 // one barrier a step parts the copies, the reads and the products of different steps, which go on side by
 // side.  X X^T of four matrices of 1003 x 4095, in us (128 steps, 41 of matrix core time): through registers
 // 102 (of which without the loads and LDS writes 57), copied and read in the step of use 98 (without the
-// copies 81, without reads and products 50).
+// copies 81, without reads and products 50), in this form 89, with matrix cores on 55% of the cycles.
 template <int KIND>
 __global__ __launch_bounds__(512, 2) void k_orth_stream(const OrthEntry *__restrict__ table, const int32_t *__restrict__ map, int tiles,
                                                         const _Float16 *__restrict__ xs, const _Float16 *__restrict__ as,
@@ -592,7 +597,7 @@ __global__ __launch_bounds__(512, 2) void k_orth_stream(const OrthEntry *__restr
 
 // A matrix of at most 64 x 64 per workgroup: norm, steps and result without leaving it.  Four waves, a
 // 32 x 32 block of each product each; X, A and the polynomial's matrix lie in LDS as two parts of rows of
-// 64 half floats.
+// 64 half floats.  A chain of fifteen products with a barrier each: 16 us for 24 matrices, 28 for 576 (32 x 32).
 __global__ __launch_bounds__(256, 3) void k_orth_small(const OrthEntry *__restrict__ table, const int32_t *__restrict__ map, int first,
                                                     int steps, double eps) {
     constexpr int PLANE = 64 * 128;

@@ -142,6 +142,7 @@ def _matrices(*rows):
     (dict(src=0), BAD), (dict(dst=0), BAD), (dict(src=MB + 2), BAD), (dict(dst=MB + 1, dtype=L.TS3_BF16), BAD),
     (dict(rows=-1), BAD), (dict(cols=-1), BAD), (dict(batch=-1), BAD), (dict(dtype=2), BAD), (dict(rows=32769), UNSUPPORTED),
     (dict(cols=32769), UNSUPPORTED), (dict(batch=1 << 24, dst=1 << 40), UNSUPPORTED),
+    (dict(rows=32768, cols=32768, batch=(1 << 31) - 1), UNSUPPORTED),
 ])
 def test_orth_refusals(row, status):
     assert L.lib().ts3_orth_matrices(_orth(), *_matrices(row), None) == status and L.lib().ts3_last_error()

@@ -254,6 +254,25 @@ def test_cross_repeats_bitwise(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_cross_first_call_captured(dtype):
+    """Enough rows for the kernels that hold all states in LDS, which need no workspace forward: a handle's
+    first call may be captured."""
+    import torch
+    from paper_2602_04940_amd import CrossAttention
+    q, k, v, _ = (to_device(t, dtype) for t in _case(1, 131_072, 64, 4, 1, 16, dtype, seed=10))
+    with CrossAttention(4, 16, 1, dtype=dtype) as a, CrossAttention(4, 16, 1, dtype=dtype) as b:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out, lse = a.forward(q, k, v)
+        for scale in (1.0, -0.5, 2.0):
+            q.mul_(scale)
+            graph.replay()
+            torch.cuda.synchronize()
+            ref, ref_lse = b.forward(q, k, v)
+            assert a.bytes() == 0 and torch.equal(out, ref) and torch.equal(lse, ref_lse), scale
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_cross_rows_are_independent(dtype):
     """A query of not-a-numbers, or a gradient of one, reaches its own row of out and dq alone."""
     import torch
