@@ -208,8 +208,11 @@ ts3_status ts3_cross_forward(ts3_cross *h, const ts3_cross_inputs *in, void *out
         auto launch = [&](auto w) -> ts3_status {
             constexpr int W = decltype(w)::value, TK = cross_tile<P, DP, W>();
             const int64_t blocks = (R + 32 * W - 1) / (32 * W), wgs = bh * blocks;
-            // as many workgroups as fit: 30,000 rows of width 32 against 2,782 states 67 us with two a unit, 37 with four
-            cross_split(A, blocks, (A.S + TK - 1) / TK, (W == 1 ? 8 : DP * P <= 32 ? 4 : 2) * cus);
+            // As many workgroups as fit: 30,000 rows of width 32 against 2,782 states 67 us with two a unit, 37 with four.
+            // With lengths, twice as many for few rows: those of long samples take as long as their own loops (4 samples
+            // of up to 100,003 states, two heads of 64: 40 against 37 us; of 128 wide, 32 states a tile, 66 against 71).
+            const int64_t units = W == 1 ? A.lengths && DP < 128 ? 16 : 8 : DP * P <= 32 ? 4 : 2;
+            cross_split(A, blocks, (A.S + TK - 1) / TK, units * cus);
             if (A.splits > 1) {
                 ts3_status r = h->part.reserve(A.splits * bh * R * (DP + 4) * 4, st, h->bytes);
                 if (r != TS3_OK) return r;

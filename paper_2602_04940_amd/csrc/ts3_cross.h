@@ -211,12 +211,16 @@ __device__ __forceinline__ int cross_length(const CrossArgs &A, int b) {
     const int n = A.lengths[b];
     return n < 0 ? 0 : n > A.S ? A.S : n;
 }
-// Which workgroup does what: (b, block of rows or states, shared head, split), the split innermost
-// and then the head, so that consecutive workgroups, which share an L2, read the same lines.
+// Which workgroup does what: (b, block of rows or states, shared head, split), the split innermost and then
+// the head.  Consecutive workgroups go to different XCDs, and so does a long sample's work: with the workgroups of
+// an L2 next to each other, the XCDs with the short samples end early (8 samples of 9,000 rows and up to 2,000
+// states, 4 heads of 64: 177 against 117 us, with the gradient 704 against 545), one row's long states come
+// through half of the XCDs (8 heads of 32 and 100,003 states 42 against 24 us), and nothing is gained (72,000 rows
+// of 2,000 states 194 against 192 us): states are few bytes a product.
 struct CrossAt {
     int b, hk, blk, split;
     __device__ __forceinline__ explicit CrossAt(const CrossArgs &A) {
-        const uint32_t i = (uint32_t)xcd_remap(blockIdx.x, gridDim.x), j = A.by_splits(i), k = A.by_heads(j), l = A.by_blocks(k);
+        const uint32_t i = blockIdx.x, j = A.by_splits(i), k = A.by_heads(j), l = A.by_blocks(k);
         split = (int)(i - j * A.by_splits.d);
         hk = (int)(j - k * A.by_heads.d);
         blk = (int)(k - l * A.by_blocks.d);
@@ -441,8 +445,8 @@ template <int P, int DP> struct CrossRows {
 
 // What bounds it: the vector ALU (50,003 float32 rows and 8 heads of 16 against 1,000 states 0.33 ms: vector
 // instructions on 72% of the cycles, most of them parting weights in three, matrix cores on 38%), and for
-// the few rows of a wave alone (W = 1) the loads of states (4 samples of 100,003, two heads of 64 each, 35 us and the
-// join's 6: 2.9 TB/s, as much as a wave and one tile ahead keep in flight).
+// the few rows of a wave alone (W = 1) the loads of states (4 samples of 100,003, two heads of 64 each, 43 us with
+// the join, 4.8 TB/s).
 //
 // Workgroup (b, hk, block, split): 32 rows per wave, W waves, against the split's tiles of
 // states.  The next tile is on its way to registers while this one is used, and goes to the other
@@ -661,7 +665,7 @@ template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_join(con
 // delta, in float32 and sum p k beside it, and dq is put right at the end by their difference; dk is
 // computed from the better delta (250,001 points of 512 states of width 32: dq off by 0.0026 of its
 // size before, by 0.0024 with it, and by 0.0017 of that from its own rounding).  There k_cross_dq_all takes
-// 0.35 ms, vector instructions on 72% of the cycles and matrix cores on 52%.  In float32 sum p k would
+// 0.34 ms, vector instructions on 71% of the cycles and matrix cores on 51%.  In float32 sum p k would
 // cost six products more, where the rounding is 2^-24.
 template <int P, int DP> struct CrossSlopes {
     using T = typename GatedIO<P>::T;
@@ -872,7 +876,7 @@ __global__ __launch_bounds__(64 * CROSS_DQ_WAVES<DP * P>, CROSS_DQ_WAVES<DP * P>
 
 // dk and dv of 32 states per wave, four waves, summed over the split's tiles of rows (queries and
 // their output gradients in LDS with the rows' lse and delta).  250,001 points and 512 states, 8 heads of 32 in
-// bfloat16: 0.35 ms, 51.7% matrix cores, 46.5% vector instructions; eight waves a compute unit and their barriers, as
+// bfloat16: 0.35 ms, matrix cores on 52% of the cycles, vector instructions on 47%; eight waves a compute unit and their barriers, as
 // many as the sums leave room for, do not hide the rest.
 template <int P, int DP> __global__ __launch_bounds__(256, DP * P <= 64 ? 2 : 1) void k_cross_dkv(const CrossArgs A) {
     using T = typename GatedIO<P>::T;
