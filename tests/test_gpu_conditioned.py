@@ -105,7 +105,8 @@ CROSS = [(1, 1, 1, 1, 1, 16), (1, 1, 700, 8, 8, 32), (2, 1, 3001, 8, 2, 64), (3,
          (2, 4, 1000, 8, 1, 16), (1, 31, 64, 2, 1, 80), (2, 33, 65, 3, 3, 32), (1, 127, 32, 4, 2, 64), (1, 130, 63, 2, 2, 112),
          (2, 129, 31, 6, 2, 96), (1, 300, 500, 2, 2, 128), (1, 257, 127, 8, 8, 16), (1, 1003, 129, 4, 1, 32),
          (1, 70, 2500, 1, 1, 64), (2, 2049, 40, 2, 2, 16), (1, 17_000, 70, 8, 8, 32), (1, 8500, 45, 16, 4, 64),
-         (1, 33_000, 33, 4, 4, 16), (2, 17_000, 97, 16, 16, 32), (1, 70_000, 40, 8, 4, 48)]
+         (1, 33_000, 33, 4, 4, 16), (2, 17_000, 97, 16, 16, 32), (1, 70_000, 40, 8, 4, 48),
+         (2, 50, 90, 16, 1, 128), (1, 9, 70, 64, 1, 32), (1, 3, 150, 1024, 1, 16), (2, 700, 3000, 32, 2, 32)]
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
