@@ -499,9 +499,10 @@ ts3_status ts3_clip_gradients(ts3_clip *h, const ts3_clip_tensor *tensors, int32
  * masked.  Where none is, out is 0 and lse minus infinity.
  *  D       : a multiple of 16 up to 128, H up to 1024; beyond: TS3_ERR_UNSUPPORTED.
  *  io_dtype: ts3_dtype of q, k, v, out and their gradients.  TS3_BF16 computes
- *            on bf16 matrix cores with float32 sums and rounds p (and, in the
- *            backward, p and ds) to bfloat16 once; TS3_FP32 keeps every operand to
- *            float32 precision in three bf16 parts.  Weights are held against a
+ *            on bf16 matrix cores with float32 sums: scores and lse are those of
+ *            float32, and p (in the backward, p and ds) is rounded to bfloat16
+ *            once; TS3_FP32 keeps every operand to float32 precision in three bf16
+ *            parts.  Weights are held against a
  *            base of up to 2^40 below their sum, so that values beyond 2^64 may
  *            overflow.
  *  scale   : finite and > 0; 0 stands for 1 / sqrt(D). */

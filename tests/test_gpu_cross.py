@@ -1,0 +1,50 @@
+"""Attention to an encoder's states on the GPU, where the shapes of test_gpu_conditioned.py do not reach
+or their bars do not see: every kernel at scores of hundreds.  Bars, fixed before the first run; u is 2^-24."""
+import math
+
+import numpy as np
+import pytest
+
+from gpu_helpers import banner, to_device, to_host
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("B,N,S,H,HK,D", [(1, 128, 40, 1, 1, 16), (1, 20, 1500, 2, 2, 16), (1, 131_072, 40, 4, 2, 16), (2, 300, 70, 2, 1, 32),
+                                          (1, 31, 900, 1, 1, 32), (1, 131_072, 70, 4, 4, 32), (1, 200, 70, 2, 2, 48), (1, 300, 40, 1, 1, 128)])
+def test_lse_of_scores_in_the_hundreds(B, N, S, H, HK, D, dtype):
+    """lse is float32 whatever the operands' type.  Every value of a query is the same, and of a state, so that errors
+    of the operands do not average out over the products.
+
+    A score is a sum of D products of bfloat16 values, exact (float32: six part products, of which those dropped and the
+    rounding of the scaled query are 4 u), times scale log2(e): 3 u; then the base, the logarithm and the way back: 4 u, of
+    the largest score X.  S weights walk S u at most, and the exponential and logarithm 4 u.
+
+    The output of values of one is one, but for the weights' rounding and its own in bfloat16, and for the walks of
+    two sums in float32, one of three part products a state, and 8 u."""
+    import torch
+    from paper_2602_04940_amd import CrossAttention
+    banner(f"lse B={B} N={N} S={S} H={H}/{HK} D={D} {dtype}")
+    scale = np.float64(np.float32(75.0 / D))
+    rng = np.random.default_rng([1, N, S, D])
+    x, y = 1 + np.arange(128) / 128, 1 + rng.integers(0, 128, (B, S, HK)) / 128
+    tt = torch.float32 if dtype == "fp32" else torch.bfloat16
+    q = to_device(x, dtype)[torch.arange(N, device="cuda") % 128][None, :, None, None].expand(B, N, H, D).contiguous()
+    k = to_device(y, dtype)[..., None].expand(B, S, HK, D).contiguous()
+    with CrossAttention(H, D, kv_heads=HK, dtype=dtype, scale=float(scale)) as a:
+        out, lse = a.forward(q, k, torch.ones_like(k))
+        torch.cuda.synchronize()
+    assert out.dtype is tt and np.abs(to_host(out) - 1).max() <= (2 * 2.0 ** -8 if dtype == "bf16" else (4 * S + 8) * U)
+    s = scale * D * x[:, None, None, None] * y[None]  # [128, B, S, HK]
+    top = s.max(axis=2, keepdims=True)
+    ref = (top + np.log(np.exp(s - top).sum(axis=2, keepdims=True)))[:, :, 0]
+    ref = np.repeat(ref.transpose(1, 2, 0), H // HK, axis=1)  # [B, H, 128]
+    X = s.max()
+    bar = ((D if dtype == "bf16" else 6 * D + 4) + 8) * U * X + (S + 4) * U
+    got = to_host(lse)
+    err = max(np.abs(got[:, :, i:i + 128] - ref[:, :, :got[:, :, i:i + 128].shape[2]]).max() for i in range(0, N, 128))
+    print(f"lse to {ref.max():.1f}: off by {err:.2e} (bar {bar:.2e})", flush=True)
+    assert err <= bar
