@@ -1,8 +1,9 @@
 // Host side of the operators of a conditioned block: attention to an encoder's states (ts3_cross.h), the
-// norms around a block (ts3_sandwich.h) and orthogonalised updates (ts3_orth.h).  Included once, after
+// norms around a block (ts3_sandwich.h) and orthogonalised updates (ts3_orth.h); how attention is cut is in
+// ts3_cross_rules.h.  Included once, after
 // ts3_train.h, for its helpers and those of ts3.hip.
 #pragma once
-#include "ts3_cross.h"
+#include "ts3_cross_rules.h"
 #include "ts3_orth.h"
 #include "ts3_sandwich.h"
 
@@ -58,8 +59,7 @@ int64_t view_extent(const ts3_view &v, int64_t B, int64_t rows, int64_t heads, i
     if (B <= 0 || rows <= 0) return 0;
     return (B - 1) * v.batch + (rows - 1) * v.row + (heads - 1) * v.head + D;
 }
-constexpr int64_t CROSS_STRIDE_MAX = int64_t(1) << 40, CROSS_ROWS_MAX = (int64_t(1) << 31) - 1024;
-constexpr int64_t CROSS_WGS_MAX = int64_t(1) << 24;  // of 256 threads: fewer than 2^32 of them
+constexpr int64_t CROSS_STRIDE_MAX = int64_t(1) << 40;
 
 ts3_status cross_check_view(const char *name, const ts3_view &v, int64_t extent, int64_t size) {
     if (extent == 0) return TS3_OK;
@@ -74,8 +74,7 @@ ts3_status cross_check_view(const char *name, const ts3_view &v, int64_t extent,
 ts3_status cross_inputs(const ts3_cross *h, const ts3_cross_inputs &in, CrossArgs &A) {
     if (in.B < 0 || in.N < 0 || in.S < 0) return fail(TS3_ERR_INVALID_ARG, "B, N and S must be >= 0");
     const int64_t B = in.B, N = in.N, S = in.S, H = h->desc.H, HK = h->desc.Hkv, D = h->desc.D;
-    if (N * (H / HK) > CROSS_ROWS_MAX || S > CROSS_ROWS_MAX || B * HK > CROSS_WGS_MAX ||
-        B * HK * ((N * (H / HK) + 31) / 32) >= CROSS_WGS_MAX || B * HK * ((S + 127) / 128) >= CROSS_WGS_MAX)
+    if (!cross_fits({B, HK, N * (H / HK), S, false}))
         return fail(TS3_ERR_UNSUPPORTED, "no launch for B=%lld, N=%lld, S=%lld", (long long)B, (long long)N, (long long)S);
     const int64_t size = h->desc.io_dtype == TS3_BF16 ? 2 : 4;
     for (const ts3_view *v : {&in.q, &in.k, &in.v}) {
@@ -105,13 +104,10 @@ ts3_status cross_overlaps(std::initializer_list<Range> ins, std::initializer_lis
     }
     return TS3_OK;
 }
-// Splits `tiles` of a loop so that the workgroups (of `blocks` blocks per sample and shared head) become
-// about `target`, each of two tiles at least.
-void cross_split(CrossArgs &A, int64_t blocks, int64_t tiles, int64_t target) {
-    const int64_t wgs = (int64_t)A.B * (A.H / A.G) * blocks;
-    const int64_t s = std::max<int64_t>(1, std::min(target / std::max<int64_t>(wgs, 1), tiles / 2));
-    A.per = (int32_t)std::max<int64_t>(1, (tiles + s - 1) / s);
-    A.splits = (int32_t)std::max<int64_t>(1, (tiles + A.per - 1) / A.per);
+CrossSize cross_size(const CrossArgs &A) { return {A.B, A.H / A.G, (int64_t)A.N * A.G, A.S, A.lengths != nullptr}; }
+void cross_cut_by(CrossArgs &A, int64_t blocks, const CrossCut &cut) {
+    A.per = (int32_t)cut.per;
+    A.splits = (int32_t)cut.splits;
     A.by_splits = CrossDiv((uint32_t)A.splits);
     A.by_blocks = CrossDiv((uint32_t)std::max<int64_t>(blocks, 1));
 }
@@ -122,15 +118,6 @@ template <int P, int DP> ts3_status cross_allow_lds(ts3_cross *h) {
     HIP_TRY(hipFuncSetAttribute((const void *)&k_cross_dq_all<P, DP>, hipFuncAttributeMaxDynamicSharedMemorySize, ATTN_LDS_MAX));
     h->lds = true;
     return TS3_OK;
-}
-
-// Workgroups per sample and shared head of the kernels that hold all states in LDS; 0 where these do not
-// fit, or where the rows are too few.
-template <typename All> int64_t cross_all(const CrossArgs &A, int64_t cus) {
-    if (!All::FITS || A.S == 0 || All::bytes(A.S) > All::LDS) return 0;
-    // A wave's blocks of 32 rows: four at least, or filling LDS and uneven ends cost more than it saves.
-    const int64_t blocks = ((int64_t)A.N * A.G + 31) / 32, bh = (int64_t)A.B * (A.H / A.G);
-    return blocks * bh < 4 * All::W * cus ? 0 : std::max<int64_t>(1, cus / bh);
 }
 
 // Tiles of a product and how many groups of waves share one, from the tiles of 128 and of 64 that there are.
@@ -203,49 +190,35 @@ ts3_status ts3_cross_forward(ts3_cross *h, const ts3_cross_inputs *in, void *out
     A.lse = lse;
     return cross_dispatch(h->desc, [&](auto p, auto dp) -> ts3_status {
         constexpr int P = decltype(p)::value, DP = decltype(dp)::value;
-        const int64_t R = (int64_t)A.N * A.G, bh = (int64_t)A.B * HK, cus = device_cu_count();
+        const int64_t R = (int64_t)A.N * A.G, bh = (int64_t)A.B * HK;
         hipStream_t st = (hipStream_t)stream;
-        auto launch = [&](auto w) -> ts3_status {
-            constexpr int W = decltype(w)::value, TK = cross_tile<P, DP, W>();
-            const int64_t blocks = (R + 32 * W - 1) / (32 * W), wgs = bh * blocks;
-            // As many workgroups as fit: 30,000 rows of width 32 against 2,782 states 67 us with two a unit, 37 with four.
-            // With lengths, twice as many for few rows: those of long samples take as long as their own loops (4 samples
-            // of up to 100,003 states, two heads of 64: 40 against 37 us; of 128 wide, 32 states a tile, 66 against 71).
-            const int64_t units = W == 1 ? A.lengths && DP < 128 ? 16 : 8 : DP * P <= 32 ? 4 : 2;
-            cross_split(A, blocks, (A.S + TK - 1) / TK, units * cus);
-            if (A.splits > 1) {
-                ts3_status r = h->part.reserve(A.splits * bh * R * (DP + 4) * 4, st, h->bytes);
-                if (r != TS3_OK) return r;
-                A.part = (float *)h->part.p;
-            }
-            hipLaunchKernelGGL((k_cross_fwd<P, DP, W>), dim3((unsigned)(wgs * A.splits)), dim3(64 * W), 0, st, A);
-            LAUNCH_CHECK("cross attention");
-            if (A.splits > 1) {
-                const int64_t count = bh * R, few = (count * (DP / 4) + 255) / 256;
-                // 12,496 rows of width 80 in two parts: 67 us in all with a workgroup a row, 45 with lanes
-                if (A.splits <= 16 && few >= cus)
-                    hipLaunchKernelGGL((k_cross_join_few<P, DP>), dim3((unsigned)few), dim3(256), 0, st, A, count);
-                else
-                    hipLaunchKernelGGL((k_cross_join<P, DP>), dim3((unsigned)count), dim3(256), 0, st, A);
-                LAUNCH_CHECK("cross attention join");
-            }
-            return TS3_OK;
-        };
-        // A wave of its own for a row or a few (float32 heads of 128 would not fit its registers).
-        if constexpr (DP * P <= 192)
-            if (R <= 32) return launch(ic<1>{});
+        const CrossPlan plan = cross_forward_plan<P, DP>(cross_size(A), device_cu_count());
+        cross_cut_by(A, plan.blocks, plan.cut);
+        const int64_t wgs = bh * plan.blocks * plan.cut.splits;
         using All = CrossAll<P, DP, 16>;
-        if constexpr (All::FITS) if (const int64_t per = cross_all<All>(A, cus); per > 0) {
+        if constexpr (All::FITS) if (plan.kind == CROSS_ALL) {
             if (ts3_status r = cross_allow_lds<P, DP>(h); r != TS3_OK) return r;
-            A.per = (int32_t)per;
-            A.splits = 1;
-            A.by_blocks = CrossDiv((uint32_t)per);
             const unsigned lds = (unsigned)All::bytes(A.S);
-            hipLaunchKernelGGL((k_cross_fwd_all<P, DP>), dim3((unsigned)(bh * per)), dim3(64 * All::W), lds, st, A);
+            hipLaunchKernelGGL((k_cross_fwd_all<P, DP>), dim3((unsigned)wgs), dim3(64 * All::W), lds, st, A);
             LAUNCH_CHECK("cross attention");
             return TS3_OK;
         }
-        return launch(ic<4>{});
+        if (plan.join != CROSS_WHOLE) {
+            ts3_status r = h->part.reserve(A.splits * bh * R * (DP + 4) * 4, st, h->bytes);
+            if (r != TS3_OK) return r;
+            A.part = (float *)h->part.p;
+        }
+        if constexpr (DP * P <= 192)
+            if (plan.kind == CROSS_ONE) hipLaunchKernelGGL((k_cross_fwd<P, DP, 1>), dim3((unsigned)wgs), dim3(64), 0, st, A);
+        if (plan.kind == CROSS_FOUR) hipLaunchKernelGGL((k_cross_fwd<P, DP, 4>), dim3((unsigned)wgs), dim3(256), 0, st, A);
+        LAUNCH_CHECK("cross attention");
+        const int64_t count = bh * R;
+        if (plan.join == CROSS_JOIN_FEW)
+            hipLaunchKernelGGL((k_cross_join_few<P, DP>), dim3((unsigned)((count * (DP / 4) + 255) / 256)), dim3(256), 0, st, A, count);
+        else if (plan.join == CROSS_JOIN)
+            hipLaunchKernelGGL((k_cross_join<P, DP>), dim3((unsigned)count), dim3(256), 0, st, A);
+        LAUNCH_CHECK("cross attention join");
+        return TS3_OK;
     });
 }
 
@@ -273,21 +246,15 @@ ts3_status ts3_cross_backward(ts3_cross *h, const ts3_cross_inputs *in, const vo
     A.out = CrossView{out, N * H * D, H * D, D};
     A.lse = const_cast<float *>(lse);
     return cross_dispatch(h->desc, [&](auto p, auto dp) -> ts3_status {
-        constexpr int P = decltype(p)::value, DP = decltype(dp)::value, T = P == 1 && DP < 128 ? 64 : 32;
-        const int64_t R = N * A.G, bh = B * HK, cus = device_cu_count();
+        constexpr int P = decltype(p)::value, DP = decltype(dp)::value;
+        const int64_t R = N * A.G, bh = B * HK;
         hipStream_t st = (hipStream_t)stream;
+        const CrossBackwardPlan plan = cross_backward_plan<P, DP>(cross_size(A), device_cu_count());
         CrossArgs Q = A, V = A;
-        const int64_t qblocks = (R + 127) / 128, vblocks = (S + 127) / 128, qwgs = bh * qblocks, vwgs = bh * vblocks;
-        cross_split(Q, qblocks, (S + T - 1) / T, 2 * cus);
+        cross_cut_by(Q, plan.qblocks, plan.q);
+        cross_cut_by(V, plan.vblocks, plan.v);
+        const int64_t qwgs = bh * plan.qblocks * plan.q.splits, vwgs = bh * plan.vblocks * plan.v.splits;
         using All = CrossAll<P, DP, CROSS_DQ_WAVES<DP * P>>;
-        const int64_t qall = cross_all<All>(A, cus);
-        if (qall > 0) {
-            Q.per = (int32_t)qall;
-            Q.splits = 1;
-            Q.by_splits = CrossDiv(1);
-            Q.by_blocks = CrossDiv((uint32_t)qall);
-        }
-        cross_split(V, vblocks, (R + T - 1) / T, (DP * P <= 48 ? 3 : 2) * cus);
         const int64_t qn = bh * R * (2 * DP + 4), vn = states * D;
         // one after the other: the parts share their memory
         const int64_t need = std::max(Q.splits > 1 ? Q.splits * qn * 4 : 0, V.splits > 1 ? 2 * V.splits * vn * 4 : 0);
@@ -298,15 +265,14 @@ ts3_status ts3_cross_backward(ts3_cross *h, const ts3_cross_inputs *in, const vo
         V.part2 = V.part + V.splits * vn;
         Q.delta = V.delta = (float *)h->delta.p;
         Q.to = dq;
-        if (R > 0 && qall > 0) {
+        if (R > 0 && plan.kind == CROSS_ALL) {
             if constexpr (All::FITS) {
                 if (ts3_status r = cross_allow_lds<P, DP>(h); r != TS3_OK) return r;
-                hipLaunchKernelGGL((k_cross_dq_all<P, DP>), dim3((unsigned)(bh * qall)), dim3(64 * All::W), (unsigned)All::bytes(S),
-                                   st, Q);
+                hipLaunchKernelGGL((k_cross_dq_all<P, DP>), dim3((unsigned)qwgs), dim3(64 * All::W), (unsigned)All::bytes(S), st, Q);
             }
             LAUNCH_CHECK("cross attention dq");
         } else if (R > 0) {
-            hipLaunchKernelGGL((k_cross_dq<P, DP>), dim3((unsigned)(qwgs * Q.splits)), dim3(256), 0, st, Q);
+            hipLaunchKernelGGL((k_cross_dq<P, DP>), dim3((unsigned)qwgs), dim3(256), 0, st, Q);
             LAUNCH_CHECK("cross attention dq");
             if (Q.splits > 1) {
                 hipLaunchKernelGGL((k_cross_sum_dq<P, DP>), dim3((unsigned)((bh * R * DP + 255) / 256)), dim3(256), 0, st, Q, bh * R);
@@ -316,7 +282,7 @@ ts3_status ts3_cross_backward(ts3_cross *h, const ts3_cross_inputs *in, const vo
         if (S > 0) {
             V.to = dk;
             V.to2 = dv;
-            hipLaunchKernelGGL((k_cross_dkv<P, DP>), dim3((unsigned)(vwgs * V.splits)), dim3(256), 0, st, V);
+            hipLaunchKernelGGL((k_cross_dkv<P, DP>), dim3((unsigned)vwgs), dim3(256), 0, st, V);
             LAUNCH_CHECK("cross attention dk and dv");
             if (V.splits > 1) {
                 hipLaunchKernelGGL((k_cross_sum<typename GatedIO<P>::T>), dim3((unsigned)((vn + 255) / 256), 2), dim3(256), 0, st, V, vn);

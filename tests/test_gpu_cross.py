@@ -1,11 +1,13 @@
 """Attention to an encoder's states on the GPU, where the shapes of test_gpu_conditioned.py do not reach
-or their bars do not see: every kernel at scores of hundreds.  Bars, fixed before the first run; u is 2^-24."""
+or their bars do not see: every kernel at scores of hundreds, many samples.  Bars, fixed before the first
+run; u is 2^-24."""
 import math
 
 import numpy as np
 import pytest
 
 from gpu_helpers import banner, to_device, to_host
+from test_gpu_conditioned import _case, _compare, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -48,3 +50,19 @@ def test_lse_of_scores_in_the_hundreds(B, N, S, H, HK, D, dtype):
     err = max(np.abs(got[:, :, i:i + 128] - ref[:, :, :got[:, :, i:i + 128].shape[2]]).max() for i in range(0, N, 128))
     print(f"lse to {ref.max():.1f}: off by {err:.2e} (bar {bar:.2e})", flush=True)
     assert err <= bar
+
+
+# (B, N, S, H, Hkv, D): more samples and shared heads than compute units, of a few rows (in the four-wave kernels)
+# and of enough that a workgroup's waves each have four blocks of them (all states in LDS).
+MANY = [(1500, 70, 50, 4, 4, 32), (4500, 1, 20, 4, 4, 16), (40, 2100, 40, 8, 8, 32), (33, 1050, 33, 16, 8, 16)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("lengths", [False, True])
+@pytest.mark.parametrize("B,N,S,H,HK,D", MANY)
+def test_many_samples(B, N, S, H, HK, D, lengths, dtype):
+    from oracle import conditioned as R
+    banner(f"cross B={B} N={N} S={S} H={H}/{HK} D={D} lengths={lengths} {dtype}")
+    q, k, v, g = _case(B, N, S, H, HK, D, dtype, seed=11)
+    lens = np.random.default_rng(12).integers(0, S + 1, B).tolist() if lengths else None
+    _compare(q, k, v, g, dtype, R.present(B, S, lens), 1 / math.sqrt(D), *_run(q, k, v, g, dtype, HK, lens))
