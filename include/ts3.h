@@ -536,8 +536,8 @@ typedef struct {
 
 /* out [B][N][H][D], contiguous and 16-byte aligned, lse float [B][H][N]; they
  * overlap no input (TS3_ERR_INVALID_ARG).  S = 0 is allowed; B = 0 or N = 0 is a
- * no-op.  TS3_ERR_UNSUPPORTED where N * H / Hkv or S reaches 2^31 - 1024, or a
- * launch 2^24 workgroups (of 32 to 256 rows).  Few points split the states over
+ * no-op.  TS3_ERR_UNSUPPORTED where N * H / Hkv or S reaches 2^31 - 1024, or B * Hkv
+ * times blocks of 128 of either 2^24 (8 heads: 268 million points).  Few points split the states over
  * workgroups, whose parts are joined in a fixed order: results repeat bitwise for
  * given sizes.  The parts' workspace grows with the calls, as the store of
  * ts3_gated_backward does. */

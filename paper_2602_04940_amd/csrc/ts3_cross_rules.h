@@ -18,10 +18,10 @@ struct CrossSize {
 constexpr int64_t CROSS_ROWS_MAX = (int64_t(1) << 31) - 1024;
 constexpr int64_t CROSS_WGS_MAX = int64_t(1) << 24;  // of 256 threads: fewer than 2^32 of them
 
-// Whether there is a launch.
+// Whether there is a launch: the most workgroups are those of four waves, 128 rows or states each.
 inline bool cross_fits(const CrossSize &c) {
     return c.R <= CROSS_ROWS_MAX && c.S <= CROSS_ROWS_MAX && c.pairs() <= CROSS_WGS_MAX &&
-           c.pairs() * ((c.R + 31) / 32) < CROSS_WGS_MAX && c.pairs() * ((c.S + 127) / 128) < CROSS_WGS_MAX;
+           c.pairs() * ((c.R + 127) / 128) < CROSS_WGS_MAX && c.pairs() * ((c.S + 127) / 128) < CROSS_WGS_MAX;
 }
 
 // A loop of tiles in `splits` parts of `per`.

@@ -68,6 +68,15 @@ def plans(tmp_path_factory):
 ONE, FOUR, ALL = 0, 1, 2
 
 
+def test_meshes_of_hundreds_of_millions_of_points_are_accepted(plans):
+    def fits(*c):
+        return plans([("bf16", *c, False)])[0]["fits"]
+    assert fits(1, 100_000_000, 512, 8, 8, 16) and fits(1, 268_435_000, 64, 8, 8, 32) and fits(1, 100_000_000, 64, 8, 1, 16)
+    assert fits(1, 8, 268_435_000, 8, 8, 32) and fits((1 << 24) - 1, 1, 128, 1, 1, 16)
+    assert not fits(1, 1 << 28, 64, 8, 8, 32) and not fits(1, 8, 1 << 28, 8, 8, 32) and not fits(1 << 24, 1, 1, 1, 1, 16)
+    assert not fits(1, (1 << 31) - 1023, 1, 1, 1, 16) and not fits(1, 1, (1 << 31) - 1023, 1, 1, 16)
+
+
 def _sizes():
     """From one sample to as many as are accepted, and from one row to many."""
     rng = random.Random(1)

@@ -1,5 +1,6 @@
 """Attention to an encoder's states on the GPU, where the shapes of test_gpu_conditioned.py do not reach
-or their bars do not see: every kernel at scores of hundreds, many samples.  Bars, fixed before the first
+or their bars do not see: every kernel at scores of hundreds, many samples, a
+mesh of 100 million points.  Bars, fixed before the first
 run; u is 2^-24."""
 import math
 
@@ -66,3 +67,44 @@ def test_many_samples(B, N, S, H, HK, D, lengths, dtype):
     q, k, v, g = _case(B, N, S, H, HK, D, dtype, seed=11)
     lens = np.random.default_rng(12).integers(0, S + 1, B).tolist() if lengths else None
     _compare(q, k, v, g, dtype, R.present(B, S, lens), 1 / math.sqrt(D), *_run(q, k, v, g, dtype, HK, lens))
+
+
+def test_a_mesh_of_100_million_points():
+    """Eight heads, whose queries (and gradients) overlap in memory: head h of point n starts 16 (n + h) elements from
+    the first.  A row depends on itself alone: blocks of points, at the ends and around the 2^26th, are bitwise as in a
+    call of their own.  dk and dv are the sums of those of five calls of 20 million points, each rounded once to
+    bfloat16 (2^-8 of its norm at most); the sums' walks are of terms of either sign, 2^-10 of the result at most."""
+    import torch
+    from paper_2602_04940_amd import CrossAttention
+    N, S, H, D = 100_000_000, 40, 8, 16
+    gen = torch.Generator(device="cuda").manual_seed(13)
+
+    def rows():
+        flat = torch.empty(16 * (N + H - 1), dtype=torch.bfloat16, device="cuda")
+        for part in flat.split(1 << 28):
+            part.copy_(torch.randn(part.shape, generator=gen, device="cuda"))
+        return flat.as_strided((1, N, H, D), (0, 16, 16, 1))
+    q, g = rows(), rows()
+    k, v = (torch.randn((1, S, H, D), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    with CrossAttention(H, D) as a, CrossAttention(H, D) as b:
+        out, lse = a.forward(q, k, v)
+        dq, dk, dv = a.backward(q, k, v, out, lse, g)
+        torch.cuda.synchronize()
+        parts = []
+        for at in range(0, N, 20_000_000):
+            s = slice(at, at + 20_000_000)
+            parts.append(b.backward(q[:, s], k, v, out[:, s].contiguous(), lse[:, :, s].contiguous(), g[:, s])[1:])
+        for at in (0, (1 << 26) - 150_000, N - 262_144):
+            s = slice(at, at + 262_144)
+            o, l = b.forward(q[:, s], k, v)
+            assert torch.equal(out[:, s], o) and torch.equal(lse[:, :, s], l), at
+            assert torch.equal(dq[:, s], b.backward(q[:, s], k, v, o, l, g[:, s])[0]), at
+        torch.cuda.synchronize()
+    del q, g, out, lse, dq, o, l
+    torch.cuda.empty_cache()
+    for got, each in ((dk, [p[0] for p in parts]), (dv, [p[1] for p in parts])):
+        got, each = got.double(), [t.double() for t in each]
+        err, size = float((got - sum(each)).norm()), float(got.norm())
+        bar = 2.0 ** -8 * (size + sum(float(t.norm()) for t in each)) + 2.0 ** -10 * size
+        print(f"off by {err:.3e} of {size:.3e} (bar {bar:.3e})", flush=True)
+        assert err <= bar
