@@ -1,6 +1,6 @@
 // Host side of the operators of a conditioned block: attention to an encoder's states (ts3_cross.h), the
-// norms around a block (ts3_sandwich.h) and orthogonalised updates (ts3_orth.h); how attention is cut is in
-// ts3_cross_rules.h.  Included once, after
+// norms around a block (ts3_sandwich.h) and orthogonalised updates (ts3_orth.h); how their calls are
+// cut is in ts3_cross_rules.h and ts3_orth_rules.h.  Included once, after
 // ts3_train.h, for its helpers and those of ts3.hip.
 #pragma once
 #include "ts3_cross_rules.h"
@@ -118,20 +118,6 @@ template <int P, int DP> ts3_status cross_allow_lds(ts3_cross *h) {
     HIP_TRY(hipFuncSetAttribute((const void *)&k_cross_dq_all<P, DP>, hipFuncAttributeMaxDynamicSharedMemorySize, ATTN_LDS_MAX));
     h->lds = true;
     return TS3_OK;
-}
-
-// Tiles of a product and how many groups of waves share one, from the tiles of 128 and of 64 that there are.
-struct OrthShape {
-    int side, groups;
-};
-// A compute unit does one tile of 128 at a time: with one to four rounds of them, the last costs more than
-// smaller tiles do, and with fewer than half a round, idle units do.  On the GPU (256 units), 128 against 64: 1,536
-// tiles of 256 K 63 against 70 us, 432 of 256 to 1,024 K 44 against 39 and of 256 K 26 against 22, 144 of
-// 4,096 K 87 against 99, 1,024 of 1,024 K 136 against 174.  Few tiles of 64 have four groups of waves each
-// (18 of 512 K 7.4 against 9 us).
-OrthShape orth_shape(int64_t large, int64_t half, int64_t cus) {
-    if (large >= cus / 2 && (large <= cus || large >= 4 * cus)) return OrthShape{128, 1};
-    return OrthShape{64, half <= cus ? 4 : 1};
 }
 
 }  // namespace
@@ -492,19 +478,7 @@ ts3_status ts3_orth_matrices(ts3_orth *h, const ts3_matrix *matrices, int32_t co
         // The longest sums first, and the small matrices behind the others.
         std::stable_sort(list.begin(), list.end(), [](const OrthEntry &p, const OrthEntry &q) { return p.c > q.c; });
         const int64_t cus = device_cu_count();
-        auto tiles = [](const OrthEntry &e, int ts, bool update) {
-            const int64_t nr = (orth_pad(e.r) + ts - 1) / ts, nc = (orth_pad(e.c) + ts - 1) / ts;
-            return e.c <= ORTH_SMALL ? 0 : e.nb * (update ? nr * nc : nr * (nr + 1) / 2);
-        };
-        OrthShape shape[2];
-        for (int u : {0, 1}) {
-            int64_t large = 0, half = 0;
-            for (const OrthEntry &e : list) {
-                large += tiles(e, 128, u);
-                half += tiles(e, 64, u);
-            }
-            shape[u] = orth_shape(large, half, cus);
-        }
+        const OrthShape shape[2] = {orth_shape(list.data(), list.size(), false, cus), orth_shape(list.data(), list.size(), true, cus)};
         int64_t x = 0, a = 0, slack = 0, n[4] = {0, 0, 0, 0}, big = 0;
         for (OrthEntry &e : list) {
             const int64_t rp = orth_pad(e.r), cp = orth_pad(e.c);
@@ -519,8 +493,8 @@ ts3_status ts3_orth_matrices(ts3_orth *h, const ts3_matrix *matrices, int32_t co
             }
             n[0] += is_small ? 1 : (int64_t)e.nb * orth_pieces((int64_t)e.r * e.c);
             n[1] += is_small ? e.nb : e.nb * (rp / 64) * (cp / 64);
-            n[2] += tiles(e, shape[0].side, false);
-            n[3] += tiles(e, shape[1].side, true);
+            n[2] += orth_tiles(e, shape[0].side, false);
+            n[3] += orth_tiles(e, shape[1].side, true);
             if (!is_small) big = n[1];
             for (int64_t k : n)
                 if (k >= int64_t(1) << 23) return fail(TS3_ERR_UNSUPPORTED, "no launch for so many or so large matrices");

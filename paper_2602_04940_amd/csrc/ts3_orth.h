@@ -24,32 +24,21 @@
 #pragma once
 #include "ts3_clip.h"   // sums of squares
 #include "ts3_cross.h"  // LDS tiles and their reads
+#include "ts3_orth_rules.h"
 
 namespace ts3 {
 
 constexpr float ORTH_A = 3.4445f, ORTH_B = -4.7750f, ORTH_C = 2.0315f;
 constexpr float ORTH_SCALE = 4096.f;  // of a value held in two half floats
 
-// A tensor of the list: nb matrices, wide form r x c, padded to rp x cp (multiples of 64).
-struct OrthEntry {
-    const void *src;
-    void *dst;
-    int64_t x, a;             // half floats before its X and its A in their buffers
-    int32_t r, c, nb, flags;  // ORTH_TURNED, ORTH_BF16
-    int32_t piece, load, gram, update;  // first workgroups of the launches
-};
 // Launches after the first.  Of a small matrix, the first does nothing but this table, and `load` is its
 // workgroup of k_orth_small.
 enum OrthLaunch { ORTH_AT_LOAD, ORTH_AT_GRAM, ORTH_AT_UPDATE };
-enum { ORTH_TURNED = 1, ORTH_BF16 = 2 };
 constexpr int ORTH_BATCH = 60;  // entries that fit a launch's arguments
 struct OrthBatch {
     OrthEntry e[ORTH_BATCH];
     int32_t count, first;  // entries before these
 };
-__host__ __device__ __forceinline__ int orth_pad(int n) { return (n + 63) & ~63; }
-
-constexpr int ORTH_SMALL = 64;  // the longer side of a matrix that one workgroup does
 
 // Pieces of a matrix that its squares are summed by.
 constexpr int64_t ORTH_PIECE = 8192;
