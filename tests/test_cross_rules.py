@@ -8,6 +8,8 @@ import subprocess
 
 import pytest
 
+from cross_shapes import FEW_PARTS, LDS_ROWS, LDS_STATES, MANY, WHOLE
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 PROGRAM = r"""
@@ -66,6 +68,7 @@ def plans(tmp_path_factory):
 
 
 ONE, FOUR, ALL = 0, 1, 2
+WHOLE_ROWS, JOIN_FEW, JOIN = 0, 1, 2
 
 
 def test_meshes_of_hundreds_of_millions_of_points_are_accepted(plans):
@@ -116,3 +119,29 @@ def test_all_states_in_lds_only_for_workgroups_with_work(plans):
                 seen.add((c[0], c[6], waves))
                 assert blocks >= 4 * waves * per, (c, p)
     assert {("bf16", 16), ("bf16", 32), ("bf16", 64), ("fp32", 16)} == {s[:2] for s in seen}
+
+
+@pytest.mark.parametrize("lengths", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_shapes_reach_what_they_are_for(plans, dtype, lengths):
+    few = plans([(dtype, *c, lengths) for c in FEW_PARTS])
+    assert all(p["kind"] == FOUR and p["join"] == JOIN_FEW and p["splits"] > 1 for p in few)
+    assert {p["DP"] for p in few} == {16, 32, 64, 128} and max(p["splits"] for p in few) >= 12
+    whole = [c for c in WHOLE if dtype == "bf16" or c[5] == 16]
+    assert all(p["kind"] == p["dq_kind"] == ALL for p in plans([(dtype, *c, lengths) for c in whole]))
+    kinds = [p["kind"] for p in plans([(dtype, *c, lengths) for c in MANY])]
+    assert kinds == ([FOUR, ONE, ALL, ALL] if dtype == "bf16" else [FOUR, ONE, FOUR, ALL])
+    B, N, H, HK = LDS_ROWS
+    for (t, D), S in LDS_STATES.items():
+        if t == dtype:
+            last, first = plans([(dtype, B, N, s, H, HK, D, lengths) for s in (S, S + 1)])
+            assert last["kind"] == last["dq_kind"] == ALL and first["kind"] == first["dq_kind"] == FOUR
+
+
+def test_shapes_of_the_first_tests_reach_the_other_kernels(plans):
+    """A wave alone, with parts joined by a workgroup; four waves, whole and in parts; dq in parts; dk and dv in parts."""
+    from test_gpu_conditioned import CROSS
+    for dtype in ("bf16", "fp32"):
+        got = plans([(dtype, *c, False) for c in CROSS])
+        assert {(p["kind"], p["join"]) for p in got} >= {(ONE, JOIN), (ONE, WHOLE_ROWS), (FOUR, WHOLE_ROWS), (FOUR, JOIN)}
+        assert {p["qsplits"] > 1 for p in got} == {p["vsplits"] > 1 for p in got} == {False, True}

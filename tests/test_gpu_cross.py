@@ -7,8 +7,9 @@ import math
 import numpy as np
 import pytest
 
+from cross_shapes import FEW_PARTS, LDS_ROWS, LDS_STATES, MANY, WHOLE, some_lengths
 from gpu_helpers import banner, to_device, to_host
-from test_gpu_conditioned import _case, _compare, _run
+from test_gpu_conditioned import _case, _check, _compare, _round, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -51,11 +52,6 @@ def test_lse_of_scores_in_the_hundreds(B, N, S, H, HK, D, dtype):
     err = max(np.abs(got[:, :, i:i + 128] - ref[:, :, :got[:, :, i:i + 128].shape[2]]).max() for i in range(0, N, 128))
     print(f"lse to {ref.max():.1f}: off by {err:.2e} (bar {bar:.2e})", flush=True)
     assert err <= bar
-
-
-# (B, N, S, H, Hkv, D): more samples and shared heads than compute units, of a few rows (in the four-wave kernels)
-# and of enough that a workgroup's waves each have four blocks of them (all states in LDS).
-MANY = [(1500, 70, 50, 4, 4, 32), (4500, 1, 20, 4, 4, 16), (40, 2100, 40, 8, 8, 32), (33, 1050, 33, 16, 8, 16)]
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
@@ -108,3 +104,114 @@ def test_a_mesh_of_100_million_points():
         bar = 2.0 ** -8 * (size + sum(float(t.norm()) for t in each)) + 2.0 ** -10 * size
         print(f"off by {err:.3e} of {size:.3e} (bar {bar:.3e})", flush=True)
         assert err <= bar
+
+
+def _close_in_norm(name, got, ref, walk):
+    """In bfloat16 every output is within 2^-8 in the mean square: its own rounding and the weights' or slopes', whose
+    terms have about its size, have at most 2^-8 / sqrt 3 each, independently (0.0033 together).  In blocks of 32 rows or
+    states, whose terms may be three times as large as their sum, within twice that and `walk`, what the float32 sums
+    may be off by: of a sample with one state dq and dk are zero, as differences of equal float32 sums.  A sum over
+    many rows that lacks one in a thousand is off by 3 %."""
+    ref = ref.reshape(-1, ref.shape[2] * ref.shape[3])
+    err = to_host(got).reshape(ref.shape) - ref
+    whole, worst = np.linalg.norm(err) / np.linalg.norm(ref), 0.0
+    for i in range(0, len(ref), 32):
+        bar = 2.0 ** -7 * np.linalg.norm(ref[i:i + 32]) + walk * math.sqrt(ref[i:i + 32].size)
+        worst = max(worst, np.linalg.norm(err[i:i + 32]) / max(bar, 1e-300))
+    print(f"{name}: {whole:.2e} in norm, worst block {worst:.3f} of its bar", flush=True)
+    assert whole <= 2.0 ** -8 and worst <= 1, name
+
+
+def _both(B, N, S, H, HK, D, dtype, lengths, seed):
+    """The bars of test_gpu_conditioned.py, of the size of the terms, and those in norm."""
+    from oracle import conditioned as R
+    banner(f"cross B={B} N={N} S={S} H={H}/{HK} D={D} lengths={lengths} {dtype}")
+    q, k, v, g = _case(B, N, S, H, HK, D, dtype, seed=seed)
+    lens = some_lengths(B, S) if lengths else None
+    there, scale = R.present(B, S, lens), 1 / math.sqrt(D)
+    out, lse, grads = _run(q, k, v, g, dtype, HK, lens)
+    refs, sizes = R.cross_backward(q, k, v, there, scale, g)
+    refs["out"], ref_lse = R.cross_forward(q, k, v, there, scale)
+    X = scale * np.sqrt((q * q).sum(3).max() * (k * k).sum(3).max())
+    walk = 8 + math.sqrt(S) + math.sqrt(N * H // HK) + (4 + math.sqrt(D)) * X
+    got, empty = to_host(lse), np.isinf(ref_lse)
+    assert (got[empty] == -np.inf).all() and np.abs(got[~empty] - ref_lse[~empty]).max() <= 4 * walk * U
+    for name, t in dict(grads, out=out).items():
+        _check(name, t, refs[name], sizes[name], dtype, walk)
+        if dtype == "bf16":
+            _close_in_norm(name, t, refs[name], 4 * walk * U * sizes[name].max())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("lengths", [False, True])
+@pytest.mark.parametrize("B,N,S,H,HK,D", FEW_PARTS)
+def test_parts_joined_by_lanes(B, N, S, H, HK, D, lengths, dtype):
+    _both(B, N, S, H, HK, D, dtype, lengths, 14)
+
+
+@pytest.mark.parametrize("lengths", [False, True])
+@pytest.mark.parametrize("B,N,S,H,HK,D,dtype", [(*c, t) for c in WHOLE for t in ("fp32", "bf16") if t == "bf16" or c[5] == 16])
+def test_all_states_in_lds(B, N, S, H, HK, D, lengths, dtype):
+    _both(B, N, S, H, HK, D, dtype, lengths, 15)
+
+
+@pytest.mark.parametrize("more", [0, 1])
+@pytest.mark.parametrize("dtype,D", LDS_STATES)
+def test_as_many_states_as_lds_holds_and_one_more(dtype, D, more):
+    """Some hundred rows of many, the last among them, against the reference of those rows alone."""
+    from oracle import conditioned as R
+    B, N, H, HK = LDS_ROWS
+    S = LDS_STATES[dtype, D] + more
+    banner(f"cross N={N} S={S} H={H}/{HK} D={D} {dtype}")
+    q, k, v, g = _case(B, N, S, H, HK, D, dtype, seed=16)
+    mask = np.random.default_rng(17).random((B, S)) < 0.9
+    mask[0, -1] = True
+    out, lse, grads = _run(q, k, v, g, dtype, HK, mask=mask)
+    rows = np.r_[0:70, np.random.default_rng(18).integers(70, N - 40, 100), N - 40:N]
+    for t in (out, grads["dq"]):
+        assert t.isfinite().all()
+    # dk and dv are sums over all rows: of these alone, in a call of their own
+    ours = _run(q[:, rows], k, v, g[:, rows], dtype, HK, mask=mask)[2]
+    _compare(q[:, rows], k, v, g[:, rows], dtype, mask, 1 / math.sqrt(D), out[:, rows], lse[:, :, rows],
+             dict(ours, dq=grads["dq"][:, rows]))
+
+
+@pytest.mark.parametrize("B,N,S,H,HK,D", [(1, 300, 40, 1, 1, 16), (2, 300, 600, 1, 1, 32), (1, 200, 700, 2, 1, 64), (1, 140_000, 40, 4, 4, 16),
+                                          (1, 500, 60, 2, 2, 128)])
+def test_bfloat16_slopes_do_not_hang_on_the_rounded_output(B, N, S, H, HK, D):
+    """Values that lie around 16 with a spread of a half: out is rounded by up to 1/16 and g.out with it, a tenth of
+    the slopes' spread.  What that would do to dq and dk is computed here and is beyond the bar; the kernels put it right
+    with float32 sums.
+
+    Bar, in norm: 2^-8 of the result, and of the root of the sum of the squares of its terms, whose roundings
+    are independent: p (dp - delta) k, delta of the rounded output, and delta's error times p k, for dq; ds q for dk."""
+    from oracle import conditioned as R
+    banner(f"cross slopes N={N} S={S} H={H}/{HK} D={D}")
+    q, k, v, g = _case(B, N, S, H, HK, D, "bf16", seed=19, scale=2.0)
+    v = np.round(4 * v).clip(-8, 8) / 8 + 16.0   # steps of 1/8: exact
+    k = k + 1.0
+    k = _round(k, "bf16")
+    there, scale = R.present(B, S), 1 / math.sqrt(D)
+    refs = R.cross_backward(q, k, v, there, scale, g)[0]
+    out, lse, grads = _run(q, k, v, g, "bf16", HK)
+    G = H // HK
+    p, _ = R.cross_weights(q, k, there, scale)
+    o = p @ R._heads(v, there, G)
+    gr, kr, vr, qr = R._rows(g), R._heads(k, there, G), R._heads(v, there, G), R._rows(q)
+    dp = gr @ vr.swapaxes(2, 3)
+    off = (gr * (_round(o, "bf16") - o)).sum(3, keepdims=True)          # of delta from the rounded output
+    ds = p * (dp - (gr * o).sum(3, keepdims=True))
+
+    def shared(t):
+        return t.reshape(B, HK, G, S, D).sum(axis=2).transpose(0, 2, 1, 3)
+    x = ds - p * off
+    terms = {"dq": scale * R._rows(np.sqrt((x * x) @ (kr * kr)) + np.abs(off) * np.sqrt((p * p) @ (kr * kr))),
+             "dk": scale * np.sqrt(shared((ds * ds).swapaxes(2, 3) @ (qr * qr)))}
+    wrong = {"dq": scale * R._rows(x @ kr), "dk": scale * shared(x.swapaxes(2, 3) @ qr)}
+    for name, t in terms.items():
+        ref = refs[name]
+        bar = 2.0 ** -8 * (np.linalg.norm(ref) + np.linalg.norm(t))
+        err, without = np.linalg.norm(to_host(grads[name]) - ref), np.linalg.norm(wrong[name] - ref)
+        print(f"{name}: off by {err / np.linalg.norm(ref):.2e} (bar {bar / np.linalg.norm(ref):.2e}, as it would be "
+              f"{without / np.linalg.norm(ref):.2e})", flush=True)
+        assert without > 1.5 * bar and err <= bar, name
