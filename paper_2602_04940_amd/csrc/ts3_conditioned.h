@@ -546,7 +546,7 @@ ts3_status ts3_orth_matrices(ts3_orth *h, const ts3_matrix *matrices, int32_t co
         auto product = [&](auto kind, const OrthShape &sh, int64_t count, const int32_t *map, const _Float16 *px, const _Float16 *pa,
                            _Float16 *out, bool last) {
             constexpr int KIND = decltype(kind)::value;
-            const auto kernel = sh.side == 128 ? &k_orth_stream<KIND> : sh.groups == 1 ? &k_orth_product<KIND, 64, 1> : &k_orth_product<KIND, 64, 4>;
+            const auto kernel = sh.side == 128 ? &k_orth_stream<KIND> : sh.groups == 1 ? &k_orth_product<KIND, 1> : &k_orth_product<KIND, 4>;
             const int64_t most = sh.side == 128 ? cus : sh.groups == 1 ? 4 * cus : count;
             const int threads = sh.side == 128 ? 512 : 256 * sh.groups;
             hipLaunchKernelGGL(kernel, dim3((unsigned)std::min(count, most)), dim3(threads), 0, st, table, map, (int)count, px, pa, out,

@@ -309,7 +309,7 @@ __device__ __forceinline__ void orth_write(const OrthJob<KIND, TS> &job, const f
         }
 }
 
-// Result tiles D[TS x TS] = sum over K of A_op B_op, K in steps of 32, four waves of TS/2 x TS/2.
+// Result tiles D[64 x 64] = sum over K of A_op B_op, K in steps of 32, four waves of 32 x 32.
 //   ORTH_GRAM    A = X X^T: both operands rows of X; the tiles on and below the diagonal, each also
 //                written mirrored
 //   ORTH_SQUARE  a I + b A + c A A: both operands rows of A (symmetric); likewise
@@ -327,11 +327,11 @@ __device__ __forceinline__ void orth_write(const OrthJob<KIND, TS> &job, const f
 // latency; those of 144 of 256 x 256 to 1024 39 and 22 us (k_orth_stream has the third: 62), with matrix cores on
 // 33 and 24% of the cycles: of a tile's four to sixteen pairs of steps the first waits for memory and an
 // epilogue follows the last.
-template <int KIND, int TS, int GROUPS>
-__global__ __launch_bounds__(256 * GROUPS, TS == 64 ? 4 : 2) void k_orth_product(const OrthEntry *__restrict__ table, const int32_t *__restrict__ map,
+template <int KIND, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS, 4) void k_orth_product(const OrthEntry *__restrict__ table, const int32_t *__restrict__ map,
                                                       int tiles, const _Float16 *__restrict__ xs,
                                                       const _Float16 *__restrict__ as, _Float16 *__restrict__ to, bool last) {
-    constexpr int NB = TS / 64;  // 32 x 32 blocks a wave's side
+    constexpr int TS = 64;
     constexpr bool UPDATE = KIND == ORTH_UPDATE;
     using Job = OrthJob<KIND, TS>;
     using TileA = OrthTile<TS, UPDATE>;
@@ -370,34 +370,23 @@ __global__ __launch_bounds__(256 * GROUPS, TS == 64 ? 4 : 2) void k_orth_product
         ta[H].store(tid, lds[H]);
         tb[H].store(tid, lds[H] + TileA::BYTES);
     };
-    f32x16 d[NB][NB];
+    f32x16 d[1][1];
     auto compute = [&](auto half) {
         const unsigned char *const al = lds[decltype(half)::value], *const bl = al + TileA::BYTES;
-        Parts<2> fa[2][NB];
-        f16x8 bh[2][NB], bo[2][NB];
+        Parts<2> fa[2];
+        f16x8 bh[2], bo[2];
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-#pragma unroll
-            for (int p = 0; p < NB; ++p) {
-                if constexpr (UPDATE) orth_cols<TS>(al, TileA::PLANE, wi * NB + p, ks, fa[ks][p]);
-                else rowsA.template read<2>(al, TileA::PLANE, wi * NB + p, ks, fa[ks][p]);
-            }
-#pragma unroll
-            for (int q = 0; q < NB; ++q) {
-                const unsigned char *const b = bl + (wj * NB + q) * 2048 + (bbase ^ (ks << 5));
-                bh[ks][q] = *reinterpret_cast<const f16x8 *>(b);
-                bo[ks][q] = *reinterpret_cast<const f16x8 *>(b + TileB::PLANE);
-            }
+            if constexpr (UPDATE) orth_cols<TS>(al, TileA::PLANE, wi, ks, fa[ks]);
+            else rowsA.template read<2>(al, TileA::PLANE, wi, ks, fa[ks]);
+            const unsigned char *const b = bl + wj * 2048 + (bbase ^ (ks << 5));
+            bh[ks] = *reinterpret_cast<const f16x8 *>(b);
+            bo[ks] = *reinterpret_cast<const f16x8 *>(b + TileB::PLANE);
         }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int t = 0; t < 3; ++t)
-#pragma unroll
-                for (int p = 0; p < NB; ++p)
-#pragma unroll
-                    for (int q = 0; q < NB; ++q)
-                        d[p][q] = mma_half(as_half(fa[ks][p].p[t == 0]), t == 1 ? bo[ks][q] : bh[ks][q], d[p][q]);
+            for (int t = 0; t < 3; ++t) d[0][0] = mma_half(as_half(fa[ks].p[t == 0]), t == 1 ? bo[ks] : bh[ks], d[0][0]);
     };
     using H0 = std::integral_constant<int, 0>;
     using H1 = std::integral_constant<int, 1>;
@@ -409,10 +398,7 @@ __global__ __launch_bounds__(256 * GROUPS, TS == 64 ? 4 : 2) void k_orth_product
     __syncthreads();
     for (;;) {
         const int then = at + gridDim.x, mine = pairs(job), rounds = (job.K / 64 + GROUPS - 1) / GROUPS;
-#pragma unroll
-        for (int p = 0; p < NB; ++p)
-#pragma unroll
-            for (int q = 0; q < NB; ++q) d[p][q] = f32x16{};
+        d[0][0] = f32x16{};
         for (int k = 0; k < rounds; ++k) {
             if (GROUPS == 1 && left == 0 && then < tiles) {
                 next = Job(table, map, xs, as, orth_tile(then, tiles));
@@ -432,27 +418,19 @@ __global__ __launch_bounds__(256 * GROUPS, TS == 64 ? 4 : 2) void k_orth_product
         }
         if constexpr (GROUPS > 1) {
             float *const sums = reinterpret_cast<float *>(&all_lds[0][0][0]) + tid;
+            if (group > 0)
 #pragma unroll
-            for (int p = 0; p < NB; ++p)
-#pragma unroll
-                for (int q = 0; q < NB; ++q)
-                    if (group > 0)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) sums[((group - 1) * NB * NB + p * NB + q) * 4096 + v * 256] = d[p][q][v];
+                for (int v = 0; v < 16; ++v) sums[(group - 1) * 4096 + v * 256] = d[0][0][v];
             __syncthreads();
             if (group > 0) return;
 #pragma unroll
-            for (int i = 0; i < GROUPS - 1; ++i)
+            for (int i = 0; i < GROUPS - 1; ++i) {
 #pragma unroll
-                for (int p = 0; p < NB; ++p)
-#pragma unroll
-                    for (int q = 0; q < NB; ++q) {
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) d[p][q][v] += sums[(i * NB * NB + p * NB + q) * 4096 + v * 256];
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
+                for (int v = 0; v < 16; ++v) d[0][0][v] += sums[i * 4096 + v * 256];
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
-        orth_write<KIND, TS, NB, NB>(job, d, as, to, last, (wi * NB) * 32, (wj * NB) * 32);
+        orth_write<KIND, TS, 1, 1>(job, d, as, to, last, wi * 32, wj * 32);
         if (GROUPS > 1 || then >= tiles) break;
         job = next;
         at = then;
