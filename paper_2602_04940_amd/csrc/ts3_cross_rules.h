@@ -45,7 +45,13 @@ template <typename All> int64_t cross_all(const CrossSize &c, int64_t cus) {
     // 2,048 samples and heads of 32 against 512 states, here and in the four-wave kernels: 256 rows each forward 139 and
     // 92 us, 512 170 and 139, 1,024 281 and 267, 2,048 500 and 520.  So a grid has less than 2^30 threads, too.
     const int64_t blocks = (c.R + 31) / 32, per = std::max<int64_t>(1, cus / c.pairs());
-    return blocks < 4 * All::W * per || blocks * c.pairs() < 4 * All::W * cus ? 0 : per;
+    if (blocks < 4 * All::W * per || blocks * c.pairs() < 4 * All::W * cus) return 0;
+    // Of the units' rounds, seven tenths at least, which the four-wave kernels' smaller workgroups fill: 32,768 rows each
+    // of 512 states, heads of 32, here and there: 264 samples and heads (0.52 of two rounds) forward 1,472 and 1,032 us,
+    // the gradient 4,051 and 3,317, 136 (0.53) 709 and 539, 1,951 and 1,773, 160 (0.63) 699 and 629, 2,028 and 1,963,
+    // 192 (0.75) 722 and 754, 2,203 and 2,217, 256 870 and 996, 2,817 and 2,991.
+    const int64_t wgs = c.pairs() * per, rounds = (wgs + cus - 1) / cus;
+    return 10 * wgs < 7 * rounds * cus ? 0 : per;
 }
 
 // CROSS_ONE: a workgroup is a wave of 32 rows; CROSS_FOUR: four waves; CROSS_ALL: all states in LDS.

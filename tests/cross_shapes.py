@@ -10,9 +10,9 @@ WHOLE = [(4, 33_000, 66, 4, 4, 32), (1, 140_000, 70, 4, 4, 64), (2, 70_000, 70, 
 # The most states that LDS holds, by type and width, with enough rows.
 LDS_STATES = {("bf16", 16): 2496, ("bf16", 32): 1216, ("bf16", 64): 576, ("fp32", 16): 832}
 LDS_ROWS = (1, 140_000, 4, 4)  # B, N, H, Hkv
-# More samples and shared heads than compute units, of a few rows (in the four-wave kernels) and of enough that a
-# workgroup's waves each have four blocks of them (all states in LDS).
-MANY = [(1500, 70, 50, 4, 4, 32), (4500, 1, 20, 4, 4, 16), (40, 2100, 40, 8, 8, 32), (33, 1050, 33, 16, 8, 16)]
+# Many samples and shared heads: of a few rows, and of enough for workgroups of four blocks a wave, but one round of them
+# and a bit (both in the four-wave kernels), or two rounds and nearly one (all states in LDS).
+MANY = [(1500, 70, 50, 4, 4, 32), (4500, 1, 20, 4, 4, 16), (33, 1050, 33, 16, 8, 16), (64, 2100, 40, 8, 8, 32), (30, 1100, 33, 16, 8, 16)]
 
 
 def some_lengths(B, S):

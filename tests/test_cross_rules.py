@@ -121,6 +121,18 @@ def test_all_states_in_lds_only_for_workgroups_with_work(plans):
     assert {("bf16", 16), ("bf16", 32), ("bf16", 64), ("fp32", 16)} == {s[:2] for s in seen}
 
 
+def test_all_states_in_lds_only_where_the_compute_units_have_work(plans):
+    """Of the rounds of workgroups, each alone on its unit, seven tenths at least."""
+    cases = [("bf16", pairs, 1 << 15, 300, 1, 1, 32, False) for pairs in range(1, 1100)]
+    taken = 0
+    for c, p in zip(cases, plans(cases)):
+        for kind, per in ((p["kind"], p["blocks"]), (p["dq_kind"], p["qblocks"])):
+            if kind == ALL:
+                taken += 1
+                assert c[1] * per >= 0.7 * 256 * -(-c[1] * per // 256), (c, p)
+    assert taken > 1100
+
+
 @pytest.mark.parametrize("lengths", [False, True])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_shapes_reach_what_they_are_for(plans, dtype, lengths):
@@ -130,7 +142,7 @@ def test_shapes_reach_what_they_are_for(plans, dtype, lengths):
     whole = [c for c in WHOLE if dtype == "bf16" or c[5] == 16]
     assert all(p["kind"] == p["dq_kind"] == ALL for p in plans([(dtype, *c, lengths) for c in whole]))
     kinds = [p["kind"] for p in plans([(dtype, *c, lengths) for c in MANY])]
-    assert kinds == ([FOUR, ONE, ALL, ALL] if dtype == "bf16" else [FOUR, ONE, FOUR, ALL])
+    assert kinds == [FOUR, ONE, FOUR, ALL if dtype == "bf16" else FOUR, ALL]
     B, N, H, HK = LDS_ROWS
     for (t, D), S in LDS_STATES.items():
         if t == dtype:
