@@ -21,7 +21,11 @@
 //   k_cross_sum, k_cross_sum_dq   sums of split gradients, in the splits' order
 //
 // Products are 32x32x16 with the operand conventions of ts3_gated.h, bfloat16 as it is (P = 1),
-// float32 as three bfloat16 parts (P = 3).  Scores are computed transposed, rows the states in
+// float32 as three bfloat16 parts (P = 3), both exactly: scores are scaled in float32, by the instruction that
+// takes the base or the logarithm of the sum from them.  (Scaled beforehand, in accumulators that start from those,
+// they would leave the matrix cores as exponents; but 16 bits of a scaled bfloat16 operand put lse off by 1.3e-3 at
+// scores of 300, and sums that start from a logarithm of 14 lose three bits of scores of one: float32 gradients were
+// off by 1.2e-6 to 1.8e-6 of their size, now by 0.7e-6, and took as long.)  Scores are computed transposed, rows the states in
 // the order of gated_row and columns the queries: a lane then holds 16 consecutive states of one
 // query, which are, as they lie, the K slots of the product with the values, and a query's
 // maximum and sum are in two lanes.  The values' operand is read from LDS transposed.
@@ -248,42 +252,6 @@ __device__ __forceinline__ void cross_load_row(const typename GatedIO<P>::T *row
     }
 }
 
-// The stationary operand of the scores.  In float32 it is scaled by scale log2(e) beforehand and parted
-// in three as the scaled value, so that the scores leave the matrix cores as exponents of two, less
-// what their accumulators start from (a maximum, or the logarithm of a sum): no vector instruction per
-// score but the exponential.  bfloat16 operands are multiplied as they are, exactly, and the float32
-// scores scaled afterwards.  Scaled beforehand and in two parts, 16 bits of them, lse was off by 1.3e-3 at scores of
-// 300 (3e-5 in this form), and 1M rows of 8 heads of 32 and 512 states took 0.87 ms (0.80).
-template <int P, int DP> struct CrossScore {
-    static constexpr bool PRE = P == 3;
-    static constexpr int KS = DP / 16;
-    Parts<P> f[KS];
-    __device__ __forceinline__ void load(const typename GatedIO<P>::T *row, int D, bool in, float scale2) {
-        const int g = (threadIdx.x & 63) >> 5;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const int c = 16 * ks + 8 * g;
-            const typename GatedIO<P>::T *const p = row + (c < D ? c : 0);
-            const bool here = in && c < D;
-            if constexpr (PRE) {
-                float v[8];
-                load8f(p, v);
-#pragma unroll
-                for (int t = 0; t < 8; ++t) v[t] *= scale2;
-                split8(v, f[ks]);
-            } else {
-                load_parts(p, f[ks]);
-            }
-            if (!(in && D == DP)) {
-                asm volatile("");  // a branch, not selections
-#pragma unroll
-                for (int q = 0; q < P; ++q) f[ks].p[q] = here ? f[ks].p[q] : bf16x8{};
-            }
-        }
-    }
-    // d += a times step ks
-    __device__ __forceinline__ void mma(f32x16 &d, const Parts<P> &a, int ks) const { mma_parts<32, P>(d, a, f[ks]); }
-};
 __device__ __forceinline__ f32x16 splat16(float v) { return f32x16{v, v, v, v, v, v, v, v, v, v, v, v, v, v, v, v}; }
 
 // Which of the tile's states from `first` are there; bit j is state first + j.
@@ -305,19 +273,17 @@ __device__ __forceinline__ unsigned char cross_mask(const CrossArgs &A, int b, i
 // precision does not depend on the base.
 template <int P, int DP> struct CrossRows {
     using T = typename GatedIO<P>::T;
-    using Score = CrossScore<P, DP>;
     static constexpr int KS = DP / 16, DB = (DP + 31) / 32;
-    Score qf;
-    f32x16 o[DB], start;  // start: minus the base, where the scores' accumulators begin
+    Parts<P> qf[KS];
+    f32x16 o[DB];
     float base, l;
     float low;  // what a sum has to reach: something while a row has no base yet, then nothing
 
     // Row r, one past the last read as the last.
     __device__ __forceinline__ void begin(const CrossArgs &A, const CrossAt &at, int r) {
-        qf.load(cross_row<T>(A.q, A, at.b, at.hk, min(r, A.rows() - 1)), A.D, true, A.scale * LOG2E);
+        cross_load_row<P, DP>(cross_row<T>(A.q, A, at.b, at.hk, min(r, A.rows() - 1)), A.D, true, qf);
         base = l = 0.f;
         low = 0x1p-16f;
-        start = f32x16{};
 #pragma unroll
         for (int d = 0; d < DB; ++d) o[d] = f32x16{};
     }
@@ -328,16 +294,15 @@ template <int P, int DP> struct CrossRows {
         f32x16 s;
         // exponents against the base, absent states' at minus infinity
         auto scores = [&]() {
-            s = Score::PRE ? start : f32x16{};
+            s = f32x16{};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 Parts<P> a;
                 rows.template read<P>(kl, plane, u, ks, a);
-                qf.mma(s, a, ks);
+                mma_parts<32, P>(s, a, qf[ks]);
             }
-            if constexpr (!Score::PRE)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) s[v] = fmaf(s[v], scale2, -base);
+            for (int v = 0; v < 16; ++v) s[v] = fmaf(s[v], scale2, -base);
             if (here != ~0u) {
                 uint32_t bits = here >> (16 * g);
                 asm("" : "+v"(bits));  // or the bits are taken apart where no state is absent, too
@@ -380,7 +345,6 @@ template <int P, int DP> struct CrossRows {
             const float alpha = have ? fast_exp2(-up) : 1.f;
             if (!moves || mx > -INFINITY) low = 0.f;
             base += up;
-            start = splat16(-base);
             l *= alpha;
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[d] *= alpha;
@@ -659,18 +623,17 @@ template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_join(con
 // cost six products more, where the rounding is 2^-24.
 template <int P, int DP> struct CrossSlopes {
     using T = typename GatedIO<P>::T;
-    using Score = CrossScore<P, DP>;
     static constexpr int KS = DP / 16, DB = (DP + 31) / 32;
     static constexpr bool MEND = P == 1;
-    Score qf;
-    Parts<P> gf[KS];
-    f32x16 o[DB], start, dstart;  // minus the logarithm of the sum, and minus delta from out
+    Parts<P> qf[KS], gf[KS];
+    f32x16 o[DB], dstart;         // dstart: minus delta from out
+    float start;                  // minus the logarithm of the sum
     f32x16 means[MEND ? DB : 1];  // sum p k
     float rest;                   // of the lane's states, sum p (dp - delta from out)
     __device__ __forceinline__ void begin(const CrossArgs &A, const CrossAt &at, int r, int g) {
         const int rc = min(r, A.rows() - 1), D = A.D;
         const T *const grow = cross_row<T>(A.g, A, at.b, at.hk, rc), *const orow = cross_row<T>(A.out, A, at.b, at.hk, rc);
-        qf.load(cross_row<T>(A.q, A, at.b, at.hk, rc), D, true, A.scale * LOG2E);
+        cross_load_row<P, DP>(cross_row<T>(A.q, A, at.b, at.hk, rc), D, true, qf);
         cross_load_row<P, DP>(grow, D, true, gf);
         float delta = 0.f;
 #pragma unroll
@@ -685,7 +648,7 @@ template <int P, int DP> struct CrossSlopes {
         }
         const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(delta), __float_as_uint(delta), false, false);
         delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-        start = splat16(-LOG2E * *cross_stat(A.lse, A, at.b, at.hk, rc));
+        start = -LOG2E * *cross_stat(A.lse, A, at.b, at.hk, rc);
         dstart = splat16(-delta);
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
@@ -697,17 +660,17 @@ template <int P, int DP> struct CrossSlopes {
     __device__ __forceinline__ void step(const unsigned char *kl, const unsigned char *vl, int plane, int u, uint32_t here,
                                          const CrossRowRead<DP> &rows, const CrossColRead<DP> &cols, float scale2, int g) {
         if (here == 0) return;
-        f32x16 s = Score::PRE ? start : f32x16{}, dp = dstart;
+        f32x16 s{}, dp = dstart;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             Parts<P> a;
             rows.template read<P>(kl, plane, u, ks, a);
-            qf.mma(s, a, ks);
+            mma_parts<32, P>(s, a, qf[ks]);
             rows.template read<P>(vl, plane, u, ks, a);
             mma_parts<32, P>(dp, a, gf[ks]);
         }
 #pragma unroll
-        for (int v = 0; v < 16; ++v) s[v] = fast_exp2(Score::PRE ? s[v] : fmaf(s[v], scale2, start[0]));
+        for (int v = 0; v < 16; ++v) s[v] = fast_exp2(fmaf(s[v], scale2, start));
         if (here != ~0u) {
             uint32_t bits = here >> (16 * g);
             asm("" : "+v"(bits));
@@ -870,7 +833,6 @@ __global__ __launch_bounds__(64 * CROSS_DQ_WAVES<DP * P>, CROSS_DQ_WAVES<DP * P>
 // many as the sums leave room for, do not hide the rest.
 template <int P, int DP> __global__ __launch_bounds__(256, DP * P <= 64 ? 2 : 1) void k_cross_dkv(const CrossArgs A) {
     using T = typename GatedIO<P>::T;
-    using Score = CrossScore<P, DP>;
     constexpr int TR = P == 1 && DP < 128 ? 64 : 32, SUB = TR / 32, KS = DP / 16, DB = (DP + 31) / 32;
     using Tile = CrossTile<P, DP, TR, 256>;
     __shared__ __align__(16) unsigned char lds[2][2][Tile::BYTES];
@@ -883,9 +845,8 @@ template <int P, int DP> __global__ __launch_bounds__(256, DP * P <= 64 ? 2 : 1)
     // a block of absent states has nothing to sum
     const int t0 = at.split * A.per, t1 = at.blk * 128 < len ? min(tiles, t0 + A.per) : t0;
     const float scale2 = A.scale * LOG2E;
-    Score kf;
-    Parts<P> vf[KS];
-    kf.load((const T *)A.k.p + at.b * A.k.sb + jc * A.k.sr + at.hk * A.k.sh, D, there, scale2);
+    Parts<P> kf[KS], vf[KS];
+    cross_load_row<P, DP>((const T *)A.k.p + at.b * A.k.sb + jc * A.k.sr + at.hk * A.k.sh, D, there, kf);
     cross_load_row<P, DP>((const T *)A.v.p + at.b * A.v.sb + jc * A.v.sr + at.hk * A.v.sh, D, there, vf);
     typename Mat<32>::D dk[DB], dv[DB];
 #pragma unroll
@@ -952,18 +913,18 @@ template <int P, int DP> __global__ __launch_bounds__(256, DP * P <= 64 ? 2 : 1)
                     dp[e + i] = y[i];
                 }
             }
-            s = Score::PRE ? ls : f32x16{};
+            s = f32x16{};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 Parts<P> a;
                 rows.template read<P>(ql, Tile::PLANE, u, ks, a);
-                kf.mma(s, a, ks);
+                mma_parts<32, P>(s, a, kf[ks]);
                 rows.template read<P>(gl, Tile::PLANE, u, ks, a);
                 mma_parts<32, P>(dp, a, vf[ks]);
             }
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                s[v] = fast_exp2(Score::PRE ? s[v] : fmaf(s[v], scale2, ls[v]));
+                s[v] = fast_exp2(fmaf(s[v], scale2, ls[v]));
                 dp[v] *= s[v];
             }
 #pragma unroll

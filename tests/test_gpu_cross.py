@@ -215,3 +215,25 @@ def test_bfloat16_slopes_do_not_hang_on_the_rounded_output(B, N, S, H, HK, D):
         print(f"{name}: off by {err / np.linalg.norm(ref):.2e} (bar {bar / np.linalg.norm(ref):.2e}, as it would be "
               f"{without / np.linalg.norm(ref):.2e})", flush=True)
         assert without > 1.5 * bar and err <= bar, name
+
+
+@pytest.mark.parametrize("D", [48, 128])
+def test_float32_weights_in_the_gradient(D):
+    """dk and dv of few rows and 5,000 states with scores below one: their errors are the weights', e^(s - lse).
+
+    lse lies in 8 to 16, and so do the logarithm before it, its multiple and the exponent: four roundings of at most
+    2^-21, uniform, one of them in nats and three times log 2, 2^-21 sqrt((1 + 3 log^2 2) / 3) = 4.3e-7 in the mean
+    square; sums of 64 rows, 24 part products of at most the result's size, 1.7e-7.  The bar is twice both.  Scores whose
+    sums of six part products per 16 of D start from the logarithm would be off by sqrt(6 D / 16) 2^-21 log 2 / sqrt 3 more:
+    1.4e-6 at 128."""
+    from oracle import conditioned as R
+    banner(f"cross float32 weights D={D}")
+    B, N, S, H = 1, 64, 5000, 8
+    q, k, v, g = _case(B, N, S, H, H, D, "fp32", seed=20, scale=0.3)
+    _, lse, grads = _run(q, k, v, g, "fp32", H)
+    assert 8 < lse.min() and lse.max() < 16 / math.log2(math.e)
+    refs = R.cross_backward(q, k, v, R.present(B, S), 1 / math.sqrt(D), g)[0]
+    for name in ("dk", "dv"):
+        err = np.linalg.norm(to_host(grads[name]) - refs[name]) / np.linalg.norm(refs[name])
+        print(f"{name}: {err:.2e} in norm", flush=True)
+        assert err <= 2 * math.hypot(4.3e-7, 1.7e-7), name
