@@ -252,6 +252,12 @@ __device__ __forceinline__ void cross_load_row(const typename GatedIO<P>::T *row
     }
 }
 
+// The sum of two lanes' values, 32 apart.
+__device__ __forceinline__ float both_halves(float v) {
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+}
+__device__ __forceinline__ float dot2(bf16x2 a, bf16x2 b, float c) { return __builtin_amdgcn_fdot2_f32_bf16(a, b, c, false); }
 __device__ __forceinline__ f32x16 splat16(float v) { return f32x16{v, v, v, v, v, v, v, v, v, v, v, v, v, v, v, v}; }
 
 // Which of the tile's states from `first` are there; bit j is state first + j.
@@ -615,12 +621,16 @@ template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_join(con
 // keys read transposed, and delta = g.out.
 //
 // In bfloat16 out is rounded, and delta from it is off by 2^-8 of |g| |out|, which where a row's weight lies on few
-// states is much of dp - delta.  It is what the slopes start from, but the loop takes sum p dp, which is
-// delta, in float32 and sum p k beside it, and dq is put right at the end by their difference; dk is
-// computed from the better delta (250,001 points of 512 states of width 32: dq off by 0.0026 of its
-// size before, by 0.0024 with it, and by 0.0017 of that from its own rounding).  There k_cross_dq_all takes
-// 0.34 ms, vector instructions on 71% of the cycles and matrix cores on 51%.  In float32 sum p k would
-// cost six products more, where the rounding is 2^-24.
+// states is much of dp - delta.  It is what the slopes x = p (dp - delta) start from, but the loop takes sum x and
+// sum p k beside sum x k, in float32: the first is what delta is off by, and dk is computed from the better one; and
+// their product is what dq is off by.  Taken from the rounded slopes instead, which sum x k has, the first also is what
+// their roundings add to dq through the mean key, as sum x k - sum x sum p k is sum x (k - mean k): keys around 4 with a
+// spread of one put dq off by 0.0070 of its size before, now by 0.0023, and keys around zero by 0.0024 and 0.0022
+// (0.0017 of it dq's own rounding).  In float32 sum p k would cost six products more, where the roundings
+// are 2^-24.
+//
+// 250,001 points of 512 states, 8 heads of 32, take k_cross_dq_all 0.35 ms, vector instructions on 78% of the cycles
+// and matrix cores on 39%.
 template <int P, int DP> struct CrossSlopes {
     using T = typename GatedIO<P>::T;
     static constexpr int KS = DP / 16, DB = (DP + 31) / 32;
@@ -629,7 +639,7 @@ template <int P, int DP> struct CrossSlopes {
     f32x16 o[DB], dstart;         // dstart: minus delta from out
     float start;                  // minus the logarithm of the sum
     f32x16 means[MEND ? DB : 1];  // sum p k
-    float rest;                   // of the lane's states, sum p (dp - delta from out)
+    float rest, rounded;          // of the lane's states, sum p (dp - delta from out), and of its roundings
     __device__ __forceinline__ void begin(const CrossArgs &A, const CrossAt &at, int r, int g) {
         const int rc = min(r, A.rows() - 1), D = A.D;
         const T *const grow = cross_row<T>(A.g, A, at.b, at.hk, rc), *const orow = cross_row<T>(A.out, A, at.b, at.hk, rc);
@@ -655,7 +665,7 @@ template <int P, int DP> struct CrossSlopes {
             o[d] = f32x16{};
             if constexpr (MEND) means[d] = f32x16{};
         }
-        rest = 0.f;
+        rest = rounded = 0.f;
     }
     __device__ __forceinline__ void step(const unsigned char *kl, const unsigned char *vl, int plane, int u, uint32_t here,
                                          const CrossRowRead<DP> &rows, const CrossColRead<DP> &cols, float scale2, int g) {
@@ -691,7 +701,11 @@ template <int P, int DP> struct CrossSlopes {
             }
             Parts<P> w, z;
             to_parts(x, w);
-            if constexpr (MEND) to_parts(y, z);
+            if constexpr (MEND) {
+                to_parts(y, z);
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) rounded = dot2(bf16x2{w.p[0][e], w.p[0][e + 1]}, bf16x2{(__bf16)1.f, (__bf16)1.f}, rounded);
+            }
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 Parts<P> a;
@@ -701,17 +715,16 @@ template <int P, int DP> struct CrossSlopes {
             }
         }
     }
-    // Parts of split loops hold sum p (dp - delta from out) k, that of p k and that without k, a row of 2 DP + 4.
+    // Parts of split loops hold sum p (dp - delta from out) k, that of p k and the two without k, a row of 2 DP + 4.
     __device__ __forceinline__ void finish(const CrossArgs &A, const CrossAt &at, int r, int g) const {
         const int R = A.rows();
-        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(rest), __float_as_uint(rest), false, false);
-        const float off = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+        const float off = both_halves(rest), sum = both_halves(rounded);
         if (r >= R) return;
         float *const part = A.part + ((((int64_t)at.split * A.B + at.b) * A.heads() + at.hk) * R + r) * (2 * DP + 4);
         T *const to = cross_to((T *)A.to, A, at.b, at.hk, r);
         if (g == 0) {
             if (A.splits == 1 || at.split == 0) *cross_stat(A.delta, A, at.b, at.hk, r) = (A.splits == 1 ? off : 0.f) - dstart[0];
-            if (A.splits > 1) part[2 * DP] = off;
+            if (MEND && A.splits > 1) part[2 * DP] = off, part[2 * DP + 1] = sum;
         }
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
@@ -721,7 +734,7 @@ template <int P, int DP> struct CrossSlopes {
             for (int v = 0; v < 16; ++v) {
                 x[v] = o[d][v];
                 if constexpr (MEND)
-                    if (A.splits == 1) x[v] -= off * means[d][v];
+                    if (A.splits == 1) x[v] -= sum * means[d][v];
                 x[v] *= A.splits == 1 ? A.scale : 1.f;
             }
             if (c >= A.D) continue;
@@ -991,17 +1004,18 @@ template <int P, int DP> __global__ __launch_bounds__(256) void k_cross_sum_dq(c
     if (bhr >= count || c >= A.D) return;
     const float *const p = A.part + bhr * (2 * DP + 4);
     const int64_t step = count * (2 * DP + 4);
-    float v = 0.f, m = 0.f, off = 0.f;
+    float v = 0.f, m = 0.f, off = 0.f, sum = 0.f;
 #pragma unroll 8
     for (int s = 0; s < A.splits; ++s) {
         v += p[s * step + c];
         if constexpr (P == 1) {
             m += p[s * step + DP + c];
             off += p[s * step + 2 * DP];
+            sum += p[s * step + 2 * DP + 1];
         }
     }
     const int b = (int)(bhr / R / A.heads()), hk = (int)(bhr / R % A.heads()), r = (int)(bhr % R);
-    cross_to((T *)A.to, A, b, hk, r)[c] = from_float<T>(A.scale * (v - off * m));
+    cross_to((T *)A.to, A, b, hk, r)[c] = from_float<T>(A.scale * (v - sum * m));
     if (P == 1 && c == 0) *cross_stat(A.delta, A, b, hk, r) += off;
 }
 

@@ -237,3 +237,29 @@ def test_float32_weights_in_the_gradient(D):
         err = np.linalg.norm(to_host(grads[name]) - refs[name]) / np.linalg.norm(refs[name])
         print(f"{name}: {err:.2e} in norm", flush=True)
         assert err <= 2 * math.hypot(4.3e-7, 1.7e-7), name
+
+
+@pytest.mark.parametrize("B,N,S,H,HK,D", [(1, 300, 40, 1, 1, 16), (2, 300, 600, 1, 1, 32), (1, 200, 700, 2, 1, 64), (1, 140_000, 40, 4, 4, 16),
+                                          (1, 500, 60, 2, 2, 128)])
+def test_bfloat16_slopes_do_not_carry_the_keys_mean(B, N, S, H, HK, D):
+    """A row's slopes sum to zero, their roundings do not: keys around 4 with a spread of one would put dq off by four
+    times as much as the keys' differences do.  The kernels take the roundings' sum times the mean key off again.
+
+    Bar, in norm: 2^-8, of which dq's own rounding and those of the terms p (dp - delta) (k - mean k), whose squares'
+    sum is about dq's, take 2^-8 / sqrt 3 each at most.  The rounded slopes' own sum is computed here, and is beyond it."""
+    from oracle import conditioned as R
+    banner(f"cross mean key N={N} S={S} H={H}/{HK} D={D}")
+    q, k, v, g = _case(B, N, S, H, HK, D, "bf16", seed=21)
+    k = _round(k + 4.0, "bf16")
+    there, scale = R.present(B, S), 1 / math.sqrt(D)
+    ref = R.cross_backward(q, k, v, there, scale, g)[0]["dq"]
+    _, _, grads = _run(q, k, v, g, "bf16", HK)
+    p, _ = R.cross_weights(q, k, there, scale)
+    G, gr = H // HK, R._rows(g)
+    kr, vr = R._heads(k, there, G), R._heads(v, there, G)
+    ds = p * (gr @ vr.swapaxes(2, 3) - (gr * (p @ vr)).sum(3, keepdims=True))
+    size = np.linalg.norm(ref)
+    err = np.linalg.norm(to_host(grads["dq"]) - ref) / size
+    without = np.linalg.norm(scale * R._rows(_round(ds, "bf16") @ kr) - ref) / size
+    print(f"dq: off by {err:.2e} (as it would be {without:.2e})", flush=True)
+    assert without > 1.2 * 2.0 ** -8 and err <= 2.0 ** -8
