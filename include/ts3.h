@@ -502,9 +502,10 @@ ts3_status ts3_clip_gradients(ts3_clip *h, const ts3_clip_tensor *tensors, int32
  *            on bf16 matrix cores with float32 sums: scores and lse are those of
  *            float32, and p (in the backward, p and ds) is rounded to bfloat16
  *            once; TS3_FP32 keeps every operand to float32 precision in three bf16
- *            parts.  Weights are held against a
- *            base of up to 2^40 below their sum, so that values beyond 2^64 may
- *            overflow.
+ *            parts.  Weights are held against a base of up to 2^40 below their
+ *            sum, so that values beyond 2^64 may overflow, and scores are float32:
+ *            beyond 2^20 in size, where their own roundings are tenths, a row's
+ *            results may be infinite or not-a-number.
  *  scale   : finite and > 0; 0 stands for 1 / sqrt(D). */
 typedef struct {
     int32_t H, Hkv, D;

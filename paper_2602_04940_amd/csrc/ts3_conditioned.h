@@ -395,7 +395,7 @@ ts3_status ts3_sandwich_backward(ts3_sandwich *h, const void *f, const void *y, 
             });
         };
         // Eight bfloat16 values a lane take 190 registers, two waves a SIMD: 1.25 ms for 1M gated rows of 256, with
-        // four 0.91; but wider rows would have two pieces a lane (500,000 of 512: 1.18 ms with eight).
+        // four 0.91; but wider rows would have two pieces a lane (500,000 of 512: 1.15 ms with eight, 3.6 TB/s).
         if constexpr (sizeof(T) == 2)
             if (h->desc.C > 256) return run(ic<8>{});
         run(ic<4>{});

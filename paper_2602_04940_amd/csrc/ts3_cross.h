@@ -403,10 +403,10 @@ template <int P, int DP> struct CrossRows {
     }
 };
 
-// What bounds it: the vector ALU (50,003 float32 rows and 8 heads of 16 against 1,000 states 0.33 ms: vector
-// instructions on 72% of the cycles, most of them parting weights in three, matrix cores on 38%), and for
-// the few rows of a wave alone (W = 1) the loads of states (4 samples of 100,003, two heads of 64 each, 43 us with
-// the join, 4.8 TB/s).
+// What bounds it: the vector ALU (50,003 float32 rows and 8 heads of 16 against 1,000 states 0.26 ms, a fifth of
+// them masked 0.28: vector instructions on 82% of the cycles, most of them parting weights in three, matrix cores on
+// 41%), and for the few rows of a wave alone (W = 1) the loads of states (one row of 4 samples of 100,003 states, two heads
+// of 64 each, 43 us with the join, 4.8 TB/s; of samples of different lengths 37 us, 3.4 TB/s, as the longest outlasts the others).
 //
 // Workgroup (b, hk, block, split): 32 rows per wave, W waves, against the split's tiles of
 // states.  The next tile is on its way to registers while this one is used, and goes to the other
@@ -475,8 +475,8 @@ __global__ __launch_bounds__(64 * W, W == 4 ? (DP * P <= 32 ? 4 : DP * P <= 96 ?
 // them.  Of the blocks, A.per workgroups (at.blk) take every one in turn, and a workgroup's waves the next
 // one each: dealt out beforehand, the waves of a SIMD, which do not run equally fast, would end
 // apart (a quarter of the waves' time idle in the forward).  1M rows of 8 heads of 32 and 512 states
-// 0.88 ms, 600 TFLOP/s: vector instructions on 76% of the cycles (an exponential, a sum and half a
-// conversion per score), matrix cores on 47%.
+// 0.79 to 0.83 ms, 640 TFLOP/s: the vector ALU is busy on all cycles (a multiply-add, an exponential, a sum and half a
+// conversion per score), matrix cores on 32%.
 template <int P, int DP, int WAVES> struct CrossAll {
     static constexpr int TK = cross_tile<P, DP, WAVES>(), W = WAVES;
     using Tile = CrossTile<P, DP, TK, 64 * W>;
@@ -842,8 +842,8 @@ __global__ __launch_bounds__(64 * CROSS_DQ_WAVES<DP * P>, CROSS_DQ_WAVES<DP * P>
 
 // dk and dv of 32 states per wave, four waves, summed over the split's tiles of rows (queries and
 // their output gradients in LDS with the rows' lse and delta).  250,001 points and 512 states, 8 heads of 32 in
-// bfloat16: 0.35 ms, matrix cores on 52% of the cycles, vector instructions on 47%; eight waves a compute unit and their barriers, as
-// many as the sums leave room for, do not hide the rest.
+// bfloat16: 0.34 ms, the vector ALU busy on 64% of the cycles, matrix cores on 40%, waves waiting for LDS on 20%: the two or
+// three waves a SIMD that the sums leave room for take turns more than they overlap.
 template <int P, int DP> __global__ __launch_bounds__(256, DP * P <= 64 ? 2 : 1) void k_cross_dkv(const CrossArgs A) {
     using T = typename GatedIO<P>::T;
     constexpr int TR = P == 1 && DP < 128 ? 64 : 32, SUB = TR / 32, KS = DP / 16, DB = (DP + 31) / 32;

@@ -210,7 +210,7 @@ __global__ __launch_bounds__(256) void k_sandwich_bwd(const SandwichGrads<T> A, 
             for (int i = 0; i < V; ++i) s[j][k][i] = 0.f;
     const int64_t step = (int64_t)gridDim.x * 4 * RW;
     // The next row's loads go out before this row's arithmetic, in bfloat16: float32, with half the arithmetic a
-    // byte, waits for memory anyway, and loses to more registers (2M rows of 128 1.30 against 1.34 ms).
+    // byte, waits for memory anyway, and loses to more registers (2M rows of 128 1.31 against 1.37 ms).
     constexpr bool EARLY = sizeof(T) == 2;
     RawPiece<T, V> rf[K], rd[K], ra[K], ry[K], re[K];
     auto fetch = [&](int64_t r0) {
